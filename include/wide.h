@@ -325,6 +325,92 @@ size_t wide_attention_decode_workspace_size(int64_t batch, int32_t L, int32_t n_
                                             int32_t group_size);
 
 /*
+ * 4-bit KV cache: quantise K and V rows as they are written.
+ *
+ * A cache row holds one (sequence, position, KV head) in
+ * wide_kv_quant_row_bytes(head_dim, quant_group) bytes: head_dim/2 bytes of
+ * 4-bit codes, then one bf16 scale per group of quant_group consecutive
+ * dimensions, then one bf16 lowest value per group.  A code c (0..15) of group
+ * g stands for low[g] + scale[g]*c.  The codes lie in 16 little-endian 32-bit
+ * words: nibble n (bits 4n..4n+3) of word l holds dimension
+ * 32*(n%4) + 2*l + n/4.
+ * Quantisation of a group: low = its least value rounded down to bf16;
+ * scale = (greatest - low)/15 rounded to nearest bf16, 0 if below 2^-126 (the
+ * group then reads back as low); code = (x - low)/scale rounded to nearest.
+ * Both roundings are decided exactly, ties to even: the same row always gives
+ * the same bytes.  A row (one head's 128 values) that holds a NaN, an infinity
+ * or a magnitude of 2^127 or more reads back as NaN.
+ *
+ *   dt        type of k and v: WIDE_BF16 or WIDE_F32.
+ *   n_seq, T  sequences, and rows of each in this call (1 when generating).
+ *   L         cache capacity (positions per sequence).
+ *   n_kv_heads, head_dim (128 only, else WIDE_ERR_UNSUPPORTED), quant_group
+ *             (32, 64 or 128).
+ *   kv_layout WIDE_KV_TOKEN_MAJOR: caches [n_seq][L][n_kv_heads][row];
+ *             WIDE_KV_HEAD_MAJOR: [n_seq][n_kv_heads][L][row].
+ *   pos       optional int32 [n_seq] (device): the position of row 0 of each
+ *             sequence; may be negative.  NULL means 0.
+ *   kv_len    optional int32 [n_seq] (device): the sequences' lengths after
+ *             this call.  NULL means L.
+ *             Row i of sequence b belongs to position pos[b] + i and is written
+ *             when 0 <= position < min(kv_len[b], L); other rows (left padding:
+ *             pos = -padding; right padding: beyond kv_len) are skipped and no
+ *             other byte of the caches changes.
+ *   k, v      [n_seq*T][n_kv_heads*head_dim], as wide_qkvo_masked writes them.
+ *   k_cache, v_cache  written; 16-byte aligned.
+ * Limit: n_seq*T*n_kv_heads < 2^31.  n_seq*T == 0 or L == 0 is a valid no-op.
+ */
+wide_status_t wide_kv_quantize(wide_dtype_t dt, int64_t n_seq, int32_t T, int32_t L,
+                               int32_t n_kv_heads, int32_t head_dim, int32_t quant_group,
+                               int32_t kv_layout, const int32_t* pos, const int32_t* kv_len,
+                               const void* k, const void* v, void* k_cache, void* v_cache,
+                               hipStream_t stream);
+
+/*
+ * 4-bit KV cache: read rows back, e.g. for wide_attention_masked against a
+ * cached prefix.  Arguments as for wide_kv_quantize, with k and v written: row
+ * i of sequence b is the cache's row at position pos[b] + i when 0 <= position
+ * < min(kv_len[b], L), else +0.  (With pos[b] = kv_len[b] - T the sequences
+ * end together and leftpad[b] = T - kv_len[b] is their padding.)
+ * low + scale*code is formed in fp32 with one rounding; bf16 rows are rounded
+ * once more.  n_seq*T == 0 is a valid no-op.
+ */
+wide_status_t wide_kv_dequantize(wide_dtype_t dt, int64_t n_seq, int32_t T, int32_t L,
+                                 int32_t n_kv_heads, int32_t head_dim, int32_t quant_group,
+                                 int32_t kv_layout, const int32_t* pos, const int32_t* kv_len,
+                                 const void* k_cache, const void* v_cache, void* k, void* v,
+                                 hipStream_t stream);
+
+/* Bytes of a cache row: head_dim/2 + 4*head_dim/quant_group (0 for sizes that
+ * wide_kv_quantize rejects). */
+size_t wide_kv_quant_row_bytes(int32_t head_dim, int32_t quant_group);
+
+/*
+ * Head-group masked attention at decode over a 4-bit cache:
+ * wide_attention_decode with k_cache and v_cache as wide_kv_quantize writes
+ * them, K and V standing for exactly the values their rows hold.
+ *   quant_group  32, 64 or 128.
+ *   kv_layout    as for wide_kv_quantize, batch for n_seq.
+ *   ws           >= wide_attention_decode_kvq_workspace_size(...) bytes.
+ *   the rest     as for wide_attention_decode (len_b = min(kv_len[b], L), len_b
+ *                <= 0 gives +0; cache rows at and past len_b are never used, nor
+ *                is the cache of a (sequence, KV head) without an active head).
+ * Limit: batch*n_q_heads < 2^24 (WIDE_ERR_UNSUPPORTED).
+ */
+wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t L,
+                                        int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                        int32_t group_size, int32_t quant_group,
+                                        const uint8_t* mask, const int32_t* kv_len,
+                                        int32_t kv_layout, const void* q, const void* k_cache,
+                                        const void* v_cache, void* o, void* ws, size_t ws_bytes,
+                                        hipStream_t stream);
+
+/* Workspace bytes for wide_attention_decode_kvq (SIZE_MAX for rejected shapes). */
+size_t wide_attention_decode_kvq_workspace_size(int64_t batch, int32_t L, int32_t n_q_heads,
+                                                int32_t n_kv_heads, int32_t head_dim,
+                                                int32_t group_size, int32_t quant_group);
+
+/*
  * Workspace bytes for wide_attention_masked (with_reorder != 0: idx/counts
  * will be NULL and the reorder is held in the workspace).  SIZE_MAX for
  * shapes wide_attention_masked would reject (causal-only checks aside).

@@ -15,7 +15,8 @@ import os
 __all__ = [
     "WideError", "lib", "wide_mask_reorder", "wide_ffn_masked", "wide_qkvo_masked", "wide_router",
     "wide_attention_masked", "wide_attention_workspace_size", "wide_attention_decode",
-    "wide_attention_decode_workspace_size", "wide_workspace_size", "wide_set_option", "wide_get_option", "wide_timing_enable",
+    "wide_attention_decode_workspace_size", "wide_kv_quantize", "wide_kv_dequantize", "wide_kv_quant_row_bytes",
+    "wide_attention_decode_kvq", "wide_attention_decode_kvq_workspace_size", "wide_workspace_size", "wide_set_option", "wide_get_option", "wide_timing_enable",
     "wide_timing_reset", "wide_timing_query", "wide_timing_filter", "wide_ffn_masked_noalloc", "wide_static_scratch_bytes", "LIB_PATH",
     "OP_REORDER", "OP_FFN", "OP_QKV", "OP_O", "OP_ROUTER", "PHASE_QKV", "PHASE_O", "F32", "BF16",
 ]
@@ -72,6 +73,17 @@ def lib() -> ctypes.CDLL:
                                             sz, vp]
         L.wide_attention_decode_workspace_size.restype = sz
         L.wide_attention_decode_workspace_size.argtypes = [i64, i32, i32, i32, i32, i32]
+        L.wide_kv_quantize.restype = ci
+        L.wide_kv_quantize.argtypes = [ci, i64, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.wide_kv_dequantize.restype = ci
+        L.wide_kv_dequantize.argtypes = [ci, i64, i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+        L.wide_kv_quant_row_bytes.restype = sz
+        L.wide_kv_quant_row_bytes.argtypes = [i32, i32]
+        L.wide_attention_decode_kvq.restype = ci
+        L.wide_attention_decode_kvq.argtypes = [ci, i64, i32, i32, i32, i32, i32, i32, vp, vp, i32, vp, vp, vp, vp,
+                                                vp, sz, vp]
+        L.wide_attention_decode_kvq_workspace_size.restype = sz
+        L.wide_attention_decode_kvq_workspace_size.argtypes = [i64, i32, i32, i32, i32, i32, i32]
         L.wide_workspace_size.restype = sz
         L.wide_workspace_size.argtypes = [ci, ci, i64, i32, i32, i32]
         L.wide_set_option.restype = ci
@@ -374,4 +386,145 @@ def wide_attention_decode(q, k_cache, v_cache, mask, n_q, n_kv, head_dim, group_
         _dtype_code(q), B, L, n_q, n_kv, head_dim, group_size, _p(mask), _p(kv_len),
         KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, _p(q), _p(k_cache),
         _p(v_cache), _p(o), _p(ws), nbytes, _stream(q)))
+    return o
+
+
+# ---- 4-bit KV cache -------------------------------------------------------------
+
+def wide_kv_quant_row_bytes(head_dim, quant_group) -> int:
+    """Bytes of one (sequence, position, KV head) row of a 4-bit cache."""
+    n = int(lib().wide_kv_quant_row_bytes(head_dim, quant_group))
+    if n == 0:
+        raise ValueError(f"no 4-bit cache with head_dim {head_dim} and quant_group {quant_group} "
+                         "(head_dim 128; quant_group 32, 64 or 128)")
+    return n
+
+
+def _gpu(first, *ts):
+    """The call's tensors, all on one GPU and contiguous; returns its device."""
+    for t in (first, *ts):
+        if t is not None and (not t.is_cuda or t.device != first.device):
+            raise ValueError("tensors must be on one GPU")
+    _contig(first, *ts)
+    return first.device
+
+
+class _on:
+    """The library launches on the current device: make it the tensors'."""
+    __slots__ = ("dev", "prev")
+
+    def __init__(self, dev):
+        self.dev = dev
+
+    def __enter__(self):
+        cuda = _torch().cuda
+        self.prev = cuda.current_device()
+        if self.prev != self.dev.index:
+            cuda.set_device(self.dev)
+
+    def __exit__(self, *exc):
+        if self.prev != self.dev.index:
+            _torch().cuda.set_device(self.prev)
+
+
+def _kv_cache_dims(k_cache, v_cache, n_kv, head_dim, quant_group, head_major):
+    """(batch, L) of a pair of 4-bit caches."""
+    row = wide_kv_quant_row_bytes(head_dim, quant_group)
+    torch = _torch()
+    for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if c.dtype != torch.uint8 or c.dim() != 4 or c.shape[3] != row or c.shape[1 if head_major else 2] != n_kv:
+            raise ValueError(f"{name} must be uint8 [batch][{'n_kv][L' if head_major else 'L][n_kv'}][{row}]")
+    if k_cache.shape != v_cache.shape:
+        raise ValueError("k_cache and v_cache differ in shape")
+    return k_cache.shape[0], k_cache.shape[2 if head_major else 1]
+
+
+def _per_seq(name, t, n):
+    if t is not None and (t.dtype != _torch().int32 or t.shape != (n,)):
+        raise ValueError(f"{name} must be int32 [{n}]")
+
+
+def wide_kv_quantize(k, v, k_cache, v_cache, n_kv, head_dim, quant_group, pos=None, kv_len=None, head_major=False):
+    """Quantise K/V rows [n_seq*T][n_kv*head_dim] (bf16 or fp32) into the 4-bit
+    caches, uint8 [n_seq][L][n_kv][row] (or [n_seq][n_kv][L][row] with
+    head_major; row = wide_kv_quant_row_bytes).  Row i of sequence b goes to
+    position pos[b] + i if 0 <= position < min(kv_len[b], L); int32 [n_seq]
+    each, None: 0 and L.  Returns (k_cache, v_cache)."""
+    dev = _gpu(k, v, k_cache, v_cache, pos, kv_len)
+    n_seq, L = _kv_cache_dims(k_cache, v_cache, n_kv, head_dim, quant_group, head_major)
+    if v.dtype != k.dtype or v.shape != k.shape or k.dim() != 2 or k.shape[1] != n_kv * head_dim:
+        raise ValueError("k and v must be [n_seq*T][n_kv*head_dim] of one dtype")
+    if k.shape[0] % n_seq if n_seq else k.shape[0]:
+        raise ValueError("k and v rows must split evenly into the caches' sequences")
+    _per_seq("pos", pos, n_seq)
+    _per_seq("kv_len", kv_len, n_seq)
+    with _on(dev):
+        _check("wide_kv_quantize", lib().wide_kv_quantize(
+            _dtype_code(k), n_seq, k.shape[0] // n_seq if n_seq else 0, L, n_kv, head_dim, quant_group,
+            KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, _p(pos), _p(kv_len), _p(k), _p(v), _p(k_cache),
+            _p(v_cache), _stream(k)))
+    return k_cache, v_cache
+
+
+def wide_kv_dequantize(k_cache, v_cache, T, n_kv, head_dim, quant_group, pos=None, kv_len=None, head_major=False,
+                       dtype=None, k=None, v=None):
+    """Rows of 4-bit caches as (k, v) [n_seq*T][n_kv*head_dim] in `dtype` (bf16
+    by default, or fp32): row i of sequence b is position pos[b] + i, +0 outside
+    [0, min(kv_len[b], L))."""
+    torch = _torch()
+    dev = _gpu(k_cache, v_cache, pos, kv_len, k, v)
+    n_seq, L = _kv_cache_dims(k_cache, v_cache, n_kv, head_dim, quant_group, head_major)
+    if T < 0:
+        raise ValueError("T must be >= 0")
+    if dtype is None:
+        dtype = torch.bfloat16 if k is None and v is None else (k if k is not None else v).dtype
+    shape = (n_seq * T, n_kv * head_dim)
+    if k is None:
+        k = torch.empty(shape, dtype=dtype, device=dev)
+    if v is None:
+        v = torch.empty(shape, dtype=dtype, device=dev)
+    if any(t.dtype != dtype or t.shape != shape for t in (k, v)):
+        raise ValueError(f"k and v must be {dtype} [{shape[0]}][{shape[1]}]")
+    _per_seq("pos", pos, n_seq)
+    _per_seq("kv_len", kv_len, n_seq)
+    with _on(dev):
+        _check("wide_kv_dequantize", lib().wide_kv_dequantize(
+            _dtype_code(k), n_seq, T, L, n_kv, head_dim, quant_group,
+            KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, _p(pos), _p(kv_len), _p(k_cache), _p(v_cache), _p(k),
+            _p(v), _stream(k)))
+    return k, v
+
+
+def wide_attention_decode_kvq_workspace_size(batch, L, n_q, n_kv, head_dim, group_size, quant_group):
+    return int(lib().wide_attention_decode_kvq_workspace_size(batch, L, n_q, n_kv, head_dim, group_size, quant_group))
+
+
+def wide_attention_decode_kvq(q, k_cache, v_cache, mask, n_q, n_kv, head_dim, group_size, quant_group, kv_len=None,
+                              o=None, ws=None, head_major=False):
+    """Head-group masked attention at decode over 4-bit caches (as
+    wide_kv_quantize leaves them).  q [B][n_q*head_dim] bf16; mask
+    [B][n_groups] uint8; kv_len optional int32 [B].  Returns o, same shape as
+    q."""
+    dev = _gpu(q, k_cache, v_cache, mask, kv_len, o, ws)
+    mask = _mask_bytes(mask)
+    B, L = _kv_cache_dims(k_cache, v_cache, n_kv, head_dim, quant_group, head_major)
+    if q.shape != (B, n_q * head_dim):
+        raise ValueError(f"q must be [{B}][{n_q * head_dim}]")
+    if group_size <= 0 or mask.shape != (B, n_q * head_dim // group_size):
+        raise ValueError("mask must be [batch][n_q*head_dim/group_size]")
+    _per_seq("kv_len", kv_len, B)
+    if o is None:
+        o = _torch().empty_like(q)
+    elif o.dtype != q.dtype or o.shape != q.shape:
+        raise ValueError("o must be like q")
+    with _on(dev):
+        if ws is None:
+            need = wide_attention_decode_kvq_workspace_size(B, L, n_q, n_kv, head_dim, group_size, quant_group)
+            # (shapes the library rejects: no workspace, the call reports why)
+            ws = None if need == SIZE_MAX else _workspace(need, dev)
+        nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+        _check("wide_attention_decode_kvq", lib().wide_attention_decode_kvq(
+            _dtype_code(q), B, L, n_q, n_kv, head_dim, group_size, quant_group, _p(mask), _p(kv_len),
+            KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, _p(q), _p(k_cache), _p(v_cache), _p(o), _p(ws), nbytes,
+            _stream(q)))
     return o

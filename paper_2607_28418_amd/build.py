@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwide.so")
 SOURCES = ["api.cpp", "reorder.hip", "gemm_mn.hip", "gemm_k.hip", "gemv.hip", "fp32.hip", "gemm256.hip", "router.hip",
-           "attention.hip", "attention_decode.hip"]
+           "attention.hip", "attention_decode.hip", "kv_quant.hip", "attention_decode_kvq.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

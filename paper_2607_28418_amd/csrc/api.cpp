@@ -1364,3 +1364,141 @@ wide_status_t wide_attention_decode(wide_dtype_t dt, int64_t batch, int32_t L, i
   if (e != hipSuccess) return hip_fail(e, "attention decode");
   return ok();
 }
+
+// ---- 4-bit KV cache ---------------------------------------------------------------
+namespace {
+
+bool kvq_group(int qg) { return qg == 32 || qg == 64 || qg == 128; }
+
+wide_status_t kvq_shape(int hd, int qg, int32_t kv_layout) {
+  if (kv_layout != WIDE_KV_TOKEN_MAJOR && kv_layout != WIDE_KV_HEAD_MAJOR)
+    return fail(WIDE_ERR_INVALID_ARG, "kv_layout must be WIDE_KV_TOKEN_MAJOR or WIDE_KV_HEAD_MAJOR");
+  if (hd <= 0) return fail(WIDE_ERR_INVALID_ARG, "head_dim must be positive");
+  if (hd != wide::kAttnHeadDim) return fail(WIDE_ERR_UNSUPPORTED, "the 4-bit cache needs head_dim 128 (got %d)", hd);
+  if (!kvq_group(qg)) return fail(WIDE_ERR_INVALID_ARG, "quant_group=%d must be 32, 64 or 128", qg);
+  return WIDE_OK;
+}
+
+// The quantiser (read = false) and the dequantiser of one call.
+wide_status_t kvq_rows(bool read, wide_dtype_t dt, int64_t n_seq, int32_t T, int32_t L, int32_t n_kv, int32_t hd,
+                       int32_t qg, int32_t kv_layout, const int32_t* pos, const int32_t* kv_len, const void* k,
+                       const void* v, const void* k_cache, const void* v_cache, hipStream_t stream) {
+  if (dt != WIDE_F32 && dt != WIDE_BF16) return fail(WIDE_ERR_INVALID_ARG, "unknown dtype %d", (int)dt);
+  if (n_seq < 0 || T < 0 || L < 0) return fail(WIDE_ERR_INVALID_ARG, "n_seq, T and L must be >= 0");
+  if (n_kv <= 0) return fail(WIDE_ERR_INVALID_ARG, "n_kv_heads must be positive");
+  constexpr int64_t lim = int64_t(1) << 31;
+  if (n_seq >= lim || (T > 0 && n_seq * T >= lim) || n_seq * T * n_kv >= lim)
+    return fail(WIDE_ERR_INVALID_ARG, "n_seq*T*n_kv_heads must be < 2^31");
+  CHECK(kvq_shape(hd, qg, kv_layout));
+  if (n_seq * T == 0 || (L == 0 && !read)) return ok();
+  CHECK(check_ptr(k, "k"));
+  CHECK(check_ptr(v, "v"));
+  if (L > 0) {
+    CHECK(check_ptr(k_cache, "k_cache"));
+    CHECK(check_ptr(v_cache, "v_cache"));
+  }
+  wide::KvqArgs a{};
+  a.k = k;
+  a.v = v;
+  a.k_cache = const_cast<void*>(k_cache);
+  a.v_cache = const_cast<void*>(v_cache);
+  a.pos = pos;
+  a.kv_len = kv_len;
+  a.n_seq = n_seq;
+  a.T = T;
+  a.L = L;
+  a.n_kv = n_kv;
+  a.ng = hd / qg;
+  a.head_major = kv_layout == WIDE_KV_HEAD_MAJOR;
+  const hipError_t e = wide::launch_kv_quant(a, dt == WIDE_F32, read, stream);
+  if (e != hipSuccess) return hip_fail(e, read ? "kv dequantize" : "kv quantize");
+  return ok();
+}
+
+wide_status_t attention_decode_kvq_shape(wide_dtype_t dt, int64_t B, int32_t L, int nq, int nkv, int hd, int G,
+                                         int qg, AttnShape& s) {
+  CHECK(attention_decode_shape(dt, B, L, nq, nkv, hd, G, s));
+  if (!kvq_group(qg)) return fail(WIDE_ERR_INVALID_ARG, "quant_group=%d must be 32, 64 or 128", qg);
+  if (B * nq >= (int64_t(1) << 24)) return fail(WIDE_ERR_UNSUPPORTED, "batch*n_q_heads must be < 2^24");
+  return WIDE_OK;
+}
+
+size_t attention_decode_kvq_ws(int64_t B, int L, int nq, int nkv) {
+  if (B == 0) return 0;
+  const int ch = wide::attn_decode_kvq_chunk(B, nkv, L);
+  const int nc = (L + ch - 1) / ch;
+  return align_up((size_t)B * nq * nc * (wide::kAttnHeadDim + 2) * sizeof(float));
+}
+
+}  // namespace
+
+size_t wide_kv_quant_row_bytes(int32_t head_dim, int32_t quant_group) {
+  if (head_dim != wide::kAttnHeadDim || !kvq_group(quant_group)) return 0;
+  return (size_t)head_dim / 2 + (size_t)(head_dim / quant_group) * 4;
+}
+
+wide_status_t wide_kv_quantize(wide_dtype_t dt, int64_t n_seq, int32_t T, int32_t L, int32_t n_kv_heads,
+                               int32_t head_dim, int32_t quant_group, int32_t kv_layout, const int32_t* pos,
+                               const int32_t* kv_len, const void* k, const void* v, void* k_cache, void* v_cache,
+                               hipStream_t stream) {
+  return kvq_rows(false, dt, n_seq, T, L, n_kv_heads, head_dim, quant_group, kv_layout, pos, kv_len, k, v, k_cache,
+                  v_cache, stream);
+}
+
+wide_status_t wide_kv_dequantize(wide_dtype_t dt, int64_t n_seq, int32_t T, int32_t L, int32_t n_kv_heads,
+                                 int32_t head_dim, int32_t quant_group, int32_t kv_layout, const int32_t* pos,
+                                 const int32_t* kv_len, const void* k_cache, const void* v_cache, void* k, void* v,
+                                 hipStream_t stream) {
+  return kvq_rows(true, dt, n_seq, T, L, n_kv_heads, head_dim, quant_group, kv_layout, pos, kv_len, k, v, k_cache,
+                  v_cache, stream);
+}
+
+size_t wide_attention_decode_kvq_workspace_size(int64_t batch, int32_t L, int32_t n_q_heads, int32_t n_kv_heads,
+                                                int32_t head_dim, int32_t group_size, int32_t quant_group) {
+  AttnShape s;
+  const std::string keep = g_last_error;
+  const bool bad = attention_decode_kvq_shape(WIDE_BF16, batch, L, n_q_heads, n_kv_heads, head_dim, group_size,
+                                              quant_group, s) != WIDE_OK;
+  g_last_error = keep;
+  return bad ? SIZE_MAX : attention_decode_kvq_ws(batch, L, n_q_heads, n_kv_heads);
+}
+
+wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t L, int32_t n_q_heads,
+                                        int32_t n_kv_heads, int32_t head_dim, int32_t group_size,
+                                        int32_t quant_group, const uint8_t* mask, const int32_t* kv_len,
+                                        int32_t kv_layout, const void* q, const void* k_cache, const void* v_cache,
+                                        void* o, void* ws, size_t ws_bytes, hipStream_t stream) {
+  AttnShape s;
+  CHECK(attention_decode_kvq_shape(dt, batch, L, n_q_heads, n_kv_heads, head_dim, group_size, quant_group, s));
+  CHECK(kvq_shape(head_dim, quant_group, kv_layout));
+  if (batch == 0) return ok();
+  CHECK(check_ptr(mask, "mask"));
+  if (kv_len) CHECK(check_ptr(kv_len, "kv_len", false));
+  CHECK(check_ptr(q, "q"));
+  CHECK(check_ptr(k_cache, "k_cache"));
+  CHECK(check_ptr(v_cache, "v_cache"));
+  CHECK(check_ptr(o, "o"));
+  CHECK(check_ws(ws, ws_bytes, attention_decode_kvq_ws(batch, L, n_q_heads, n_kv_heads)));
+  wide::AttnDecArgs a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(k_cache);
+  a.v = static_cast<const uint16_t*>(v_cache);
+  a.o = static_cast<uint16_t*>(o);
+  a.mask = mask;
+  a.kv_len = kv_len;
+  a.part = static_cast<float*>(ws);
+  a.B = (int)batch;
+  a.L = L;
+  a.n_q = n_q_heads;
+  a.n_kv = n_kv_heads;
+  a.ng = s.ng;
+  a.hpg = s.hpg;
+  a.qpk = s.qpk;
+  a.head_major = kv_layout == WIDE_KV_HEAD_MAJOR;
+  a.chunk = wide::attn_decode_kvq_chunk(batch, n_kv_heads, L);
+  a.n_chunks = (L + a.chunk - 1) / a.chunk;
+  a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
+  const hipError_t e = wide::launch_attention_decode_kvq(a, head_dim / quant_group, stream);
+  if (e != hipSuccess) return hip_fail(e, "attention decode, 4-bit cache");
+  return ok();
+}

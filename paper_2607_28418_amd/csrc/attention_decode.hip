@@ -462,6 +462,10 @@ hipError_t launch_attention_decode(AttnDecArgs a, hipStream_t s) {
 #undef WIDE_DEC
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  return launch_attention_decode_merge(a, s);
+}
+
+hipError_t launch_attention_decode_merge(const AttnDecArgs& a, hipStream_t s) {
   const int heads = a.B * a.n_q;
   const bool wide_merge = a.n_chunks > (heads <= 1024 ? 4 : 8) &&
                           (heads <= 2048 || (a.table && a.waves >= 4 * a.B * a.n_kv));

@@ -292,6 +292,25 @@ int attn_decode_chunk(int B, int n_kv, int L);
 constexpr int kAttnDecMaxPairs = 2016, kAttnDecWaves = 2048;
 int attn_decode_waves(int64_t B, int n_kv, int L);  // 0: no balanced split for this shape
 hipError_t launch_attention_decode(AttnDecArgs a, hipStream_t s);
+// The second kernel: one pair's partials to o (also run over the 4-bit cache's).
+hipError_t launch_attention_decode_merge(const AttnDecArgs& a, hipStream_t s);
+
+// ---- 4-bit KV cache (kv_quant.hip, attention_decode_kvq.hip)
+struct KvqArgs {
+  const void* k;            // [n_seq*T][n_kv*128] bf16 or fp32 (written by the dequantiser)
+  const void* v;
+  void* k_cache;            // rows of 64 + 4*ng bytes: [n_seq][L][n_kv], or [n_seq][n_kv][L] if head_major
+  void* v_cache;
+  const int32_t* pos;       // optional [n_seq]: position of each sequence's row 0 (NULL: 0)
+  const int32_t* kv_len;    // optional [n_seq]: rows at positions [0, min(kv_len, L)) count (NULL: L)
+  int64_t n_seq;
+  int T, L, n_kv, ng;       // ng = 128 / quant_group: 1, 2 or 4
+  int head_major;
+};
+hipError_t launch_kv_quant(const KvqArgs& a, bool f32, bool read, hipStream_t s);
+// a.k and a.v are the 4-bit caches; quant_groups per row: 1, 2 or 4
+int attn_decode_kvq_chunk(int64_t B, int n_kv, int L);
+hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStream_t s);
 
 hipError_t launch_gemv_n(const GVNArgs& a, bool swiglu, hipStream_t s);
 hipError_t launch_gemv_k(const GVKArgs& a, hipStream_t s);
