@@ -1420,6 +1420,7 @@ wide_status_t attention_decode_kvq_shape(wide_dtype_t dt, int64_t B, int32_t L, 
   CHECK(attention_decode_shape(dt, B, L, nq, nkv, hd, G, s));
   if (!kvq_group(qg)) return fail(WIDE_ERR_INVALID_ARG, "quant_group=%d must be 32, 64 or 128", qg);
   if (B * nq >= (int64_t(1) << 24)) return fail(WIDE_ERR_UNSUPPORTED, "batch*n_q_heads must be < 2^24");
+  if (nkv > 65536) return fail(WIDE_ERR_UNSUPPORTED, "more than 65536 KV heads");
   return WIDE_OK;
 }
 
