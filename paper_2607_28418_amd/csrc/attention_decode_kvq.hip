@@ -46,10 +46,12 @@ __device__ __forceinline__ f32x4 mfma16k16(u32x2 a, u32x2 b, f32x4 c) {
 }
 
 // Two codes (nibble N of either half of w, N = 0..3) as the bf16 pair 16 + c.
+// The exponents come in a register: an and-or with two literals or two scalars
+// is two instructions.
 template <int N>
-__device__ __forceinline__ uint32_t codes(uint32_t w) {
+__device__ __forceinline__ uint32_t codes(uint32_t w, uint32_t sixteens) {
   const uint32_t x = N == 0 ? w << 3 : w >> (4 * N - 3);
-  return (x & 0x00780078u) | 0x41804180u;
+  return (x & 0x00780078u) | sixteens;
 }
 
 // The (scale, low) words of a row as a 16x16x16 operand.  NG = 4: lanes with an
@@ -73,7 +75,7 @@ struct Tile {
 
 // W16: 9..16 query heads per KV head (both parts of p s in MFMAs of their own).
 template <int NG, bool W16, int NW>
-__global__ __launch_bounds__(NW * 64) void wide_attn_decode_kvq(AttnDecArgs a) {
+__global__ __launch_bounds__(NW * 64, 2) void wide_attn_decode_kvq(AttnDecArgs a) {
   constexpr int R = 64 + 4 * NG;       // bytes of a cache row
   constexpr int H = W16 ? 16 : 8;
   constexpr int GQ = 4 / NG;           // 32-wide groups per quantisation group
@@ -205,6 +207,8 @@ __global__ __launch_bounds__(NW * 64) void wide_attn_decode_kvq(AttnDecArgs a) {
 #pragma unroll
   for (int n = 0; n < 8; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
+  uint32_t sixteens = 0x41804180u;
+  asm("" : "+v"(sixteens));
   const float second = !W16 && l16 >= 8 ? 1.0f : 0.0f;
 
   auto process = [&](int j, const Tile<NG>& T) {
@@ -219,8 +223,8 @@ __global__ __launch_bounds__(NW * 64) void wide_attn_decode_kvq(AttnDecArgs a) {
         u32x4 A;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          A[i] = g == 0 ? codes<0>(T.kc[t][i]) : g == 1 ? codes<1>(T.kc[t][i]) : g == 2 ? codes<2>(T.kc[t][i])
-                                                                                          : codes<3>(T.kc[t][i]);
+          A[i] = g == 0 ? codes<0>(T.kc[t][i], sixteens) : g == 1 ? codes<1>(T.kc[t][i], sixteens) : g == 2 ? codes<2>(T.kc[t][i], sixteens)
+                                                                                          : codes<3>(T.kc[t][i], sixteens);
         D[g / GQ] = mfma16(A, qf[g], g % GQ == 0 ? zero : D[g / GQ]);
       }
 #pragma unroll
@@ -230,7 +234,8 @@ __global__ __launch_bounds__(NW * 64) void wide_attn_decode_kvq(AttnDecArgs a) {
         for (int r = 0; r < 4; ++r) S[t][r] = fmaf(D[g][r], s[r], S[t][r]);
       }
     }
-    if (j + kTile > j1) {
+    if (j + kTile > j1) {  // the last tile
+      asm volatile("");    // (a branch, not sixteen instructions in every tile)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -292,7 +297,7 @@ __global__ __launch_bounds__(NW * 64) void wide_attn_decode_kvq(AttnDecArgs a) {
               y[r] = x[r] - hi;
               x[r] = hi;
             } else {
-              x[r] = fabsf(fmaf(second, x[r], -hi));  // hi, or x - hi
+              x[r] = fmaf(second, x[r], -hi);  // -hi, or x - hi
             }
           }
 #pragma unroll
@@ -305,8 +310,8 @@ __global__ __launch_bounds__(NW * 64) void wide_attn_decode_kvq(AttnDecArgs a) {
       u32x4 B0, B1;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        B0[i] = g == 0 ? codes<0>(vl[i]) : g == 1 ? codes<1>(vl[i]) : g == 2 ? codes<2>(vl[i]) : codes<3>(vl[i]);
-        B1[i] = g == 0 ? codes<0>(vh[i]) : g == 1 ? codes<1>(vh[i]) : g == 2 ? codes<2>(vh[i]) : codes<3>(vh[i]);
+        B0[i] = g == 0 ? codes<0>(vl[i], sixteens) : g == 1 ? codes<1>(vl[i], sixteens) : g == 2 ? codes<2>(vl[i], sixteens) : codes<3>(vl[i], sixteens);
+        B1[i] = g == 0 ? codes<0>(vh[i], sixteens) : g == 1 ? codes<1>(vh[i], sixteens) : g == 2 ? codes<2>(vh[i], sixteens) : codes<3>(vh[i], sixteens);
       }
       acc[g] = mfma16(A, B0, acc[g]);
       acc[4 + g] = mfma16(A, B1, acc[4 + g]);
@@ -324,14 +329,13 @@ __global__ __launch_bounds__(NW * 64) void wide_attn_decode_kvq(AttnDecArgs a) {
     Tile<NG> t0, t1;
     load(j, t0);
     load(j + kStep, t1);
-    for (; j < j1; j += 2 * kStep) {
+    for (; j + kStep < j1; j += 2 * kStep) {
       process(j, t0);
       load(j + 2 * kStep, t0);
-      if (j + kStep < j1) {
-        process(j + kStep, t1);
-        load(j + 3 * kStep, t1);
-      }
+      process(j + kStep, t1);
+      load(j + 3 * kStep, t1);
     }
+    if (j < j1) process(j, t0);
   }
 
   // ---- the waves' results meet
@@ -353,7 +357,7 @@ __global__ __launch_bounds__(NW * 64) void wide_attn_decode_kvq(AttnDecArgs a) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float x = acc[n][r];
-      if (!W16) x += __shfl_xor(x, 32);  // the two parts of p s
+      if (!W16) x = __shfl_xor(x, 32) - x;  // the two parts of p s: -hi in the rows below 8
       const int h = W16 ? 4 * g4 + r : 4 * (g4 & 1) + r;
       if (W16 || g4 < 2) s_o[w][h][32 * (n & 3) + 2 * l16 + (n >> 2)] = x;
     }
