@@ -395,7 +395,8 @@ size_t wide_kv_quant_row_bytes(int32_t head_dim, int32_t quant_group);
  *   the rest     as for wide_attention_decode (len_b = min(kv_len[b], L), len_b
  *                <= 0 gives +0; cache rows at and past len_b are never used, nor
  *                is the cache of a (sequence, KV head) without an active head).
- * Limit: batch*n_q_heads < 2^24 (WIDE_ERR_UNSUPPORTED).
+ * Limits (WIDE_ERR_UNSUPPORTED): batch*n_q_heads < 2^24, n_kv_heads <= 65536,
+ * L <= 2^30.
  */
 wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t L,
                                         int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,

@@ -1421,14 +1421,24 @@ wide_status_t attention_decode_kvq_shape(wide_dtype_t dt, int64_t B, int32_t L, 
   if (!kvq_group(qg)) return fail(WIDE_ERR_INVALID_ARG, "quant_group=%d must be 32, 64 or 128", qg);
   if (B * nq >= (int64_t(1) << 24)) return fail(WIDE_ERR_UNSUPPORTED, "batch*n_q_heads must be < 2^24");
   if (nkv > 65536) return fail(WIDE_ERR_UNSUPPORTED, "more than 65536 KV heads");
+  if (L > (1 << 30)) return fail(WIDE_ERR_UNSUPPORTED, "L must be <= 2^30");
   return WIDE_OK;
 }
 
-size_t attention_decode_kvq_ws(int64_t B, int L, int nq, int nkv) {
+// Workspace of a call whose waves share the work: the pairs' segments, then the
+// segments' partials (the table alone, unused, otherwise).
+struct KvqWS {
+  int waves = 0;
+  int32_t* table = nullptr;
+  float* part = nullptr;
+};
+size_t carve_attention_decode_kvq(Carve& c, int64_t B, int L, int nq, int nkv, KvqWS& w) {
   if (B == 0) return 0;
-  const int ch = wide::attn_decode_kvq_chunk(B, nkv, L);
-  const int nc = (L + ch - 1) / ch;
-  return align_up((size_t)B * nq * nc * (wide::kAttnHeadDim + 2) * sizeof(float));
+  w.waves = wide::attn_decode_kvq_waves(B, nkv, L);
+  w.table = c.take<int32_t>((size_t)B * nkv * 2);
+  if (w.waves) w.part = c.take<float>(wide::attn_decode_kvq_part_floats(B, nkv, nq / nkv, w.waves));
+  else w.table = nullptr;
+  return c.off;
 }
 
 }  // namespace
@@ -1461,7 +1471,9 @@ size_t wide_attention_decode_kvq_workspace_size(int64_t batch, int32_t L, int32_
   const bool bad = attention_decode_kvq_shape(WIDE_BF16, batch, L, n_q_heads, n_kv_heads, head_dim, group_size,
                                               quant_group, s) != WIDE_OK;
   g_last_error = keep;
-  return bad ? SIZE_MAX : attention_decode_kvq_ws(batch, L, n_q_heads, n_kv_heads);
+  Carve c(nullptr);
+  KvqWS w;
+  return bad ? SIZE_MAX : carve_attention_decode_kvq(c, batch, L, n_q_heads, n_kv_heads, w);
 }
 
 wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t L, int32_t n_q_heads,
@@ -1479,7 +1491,13 @@ wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t 
   CHECK(check_ptr(k_cache, "k_cache"));
   CHECK(check_ptr(v_cache, "v_cache"));
   CHECK(check_ptr(o, "o"));
-  CHECK(check_ws(ws, ws_bytes, attention_decode_kvq_ws(batch, L, n_q_heads, n_kv_heads)));
+  KvqWS w;
+  {
+    Carve c0(nullptr);
+    CHECK(check_ws(ws, ws_bytes, carve_attention_decode_kvq(c0, batch, L, n_q_heads, n_kv_heads, w)));
+  }
+  Carve c(ws);
+  carve_attention_decode_kvq(c, batch, L, n_q_heads, n_kv_heads, w);
   wide::AttnDecArgs a{};
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k_cache);
@@ -1487,7 +1505,9 @@ wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t 
   a.o = static_cast<uint16_t*>(o);
   a.mask = mask;
   a.kv_len = kv_len;
-  a.part = static_cast<float*>(ws);
+  a.part = w.part;
+  a.table = w.table;
+  a.waves = w.waves;
   a.B = (int)batch;
   a.L = L;
   a.n_q = n_q_heads;
@@ -1496,8 +1516,6 @@ wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t 
   a.hpg = s.hpg;
   a.qpk = s.qpk;
   a.head_major = kv_layout == WIDE_KV_HEAD_MAJOR;
-  a.chunk = wide::attn_decode_kvq_chunk(batch, n_kv_heads, L);
-  a.n_chunks = (L + a.chunk - 1) / a.chunk;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
   const hipError_t e = wide::launch_attention_decode_kvq(a, head_dim / quant_group, stream);
   if (e != hipSuccess) return hip_fail(e, "attention decode, 4-bit cache");

@@ -30,6 +30,7 @@
 #include <algorithm>
 
 #include "common.h"
+#include "decode_split.h"
 #include "kernels.h"
 #include "launch.h"
 #include "tile256.h"
@@ -38,7 +39,7 @@ namespace wide {
 namespace {
 
 constexpr int kHd = 128;
-constexpr int kDT = 256;    // threads per workgroup: 4 independent waves
+constexpr int kDT = kSplitThreads;  // threads per workgroup: 4 independent waves
 constexpr int kU = 16;      // keys per unit
 constexpr int kDepth = 3;   // units in flight per wave
 
@@ -56,80 +57,7 @@ struct Unit {
   u32x4 v[4];  // lane: key 4i + lane/16, dims 8*(lane%16) .. +8
 };
 
-// Active query heads of (sequence b, KV head hkv): bit i = head hkv*qpk + i.
-__device__ __forceinline__ uint32_t active_heads(const AttnDecArgs& a, int b, int hkv) {
-  const uint8_t* mrow = a.mask + (int64_t)b * a.ng;
-  uint32_t act = 0;
-  for (int i = 0; i < a.qpk; ++i)
-    if (mrow[(hkv * a.qpk + i) / a.hpg]) act |= 1u << i;
-  return act;
-}
-__device__ __forceinline__ int seq_len(const AttnDecArgs& a, int b) {
-  return a.kv_len ? min(a.kv_len[b], a.L) : a.L;
-}
-
-// Balanced split.  What a token reads depends on the mask and on its
-// sequence's length, both known on the device only, so cutting every
-// (sequence, KV head) pair into equal chunks leaves some CUs with several
-// times the work of others.  Here every workgroup first lists the pairs'
-// 16-key units (0 for a pair no head of which is active) as a prefix sum in
-// LDS; with U units in all, wave i of a.waves (one round of resident waves)
-// takes units [i q, (i + 1) q), q = max(ceil(U / waves), kMinUnits), which may
-// cross from one pair into the next.  Each (wave, pair) segment leaves one
-// partial result, in slot i + (active pairs before the pair); workgroup 0
-// writes every pair's first slot and segment count for the merge.
-// Ragged caches, 32 sequences of up to 8192 keys, half the KV heads active:
-// kernel 91 -> 69 us; nothing ragged, all heads active: 201 -> 197.
-constexpr int kMinUnits = 4;  // 64 keys
-
-constexpr uint64_t kUnitBits = (1ull << 40) - 1;  // of a prefix: units; above them: active pairs
-
-__device__ __forceinline__ void list_units(const AttnDecArgs& a, uint64_t* s_pre, uint64_t* s_sum) {
-  const int tid = threadIdx.x, w = wave_id(), lane = lane_id();
-  const int P = a.B * a.n_kv, per = (P + kDT - 1) / kDT;
-  const int p0 = min(P, tid * per), p1 = min(P, p0 + per);
-  uint64_t sum = 0;  // active pairs << 40 | units
-  for (int p = p0; p < p1; ++p) {
-    const int b = p / a.n_kv, h0 = (p - b * a.n_kv) * a.qpk;
-    const uint8_t* mrow = a.mask + (int64_t)b * a.ng;
-    const int g0 = h0 / a.hpg, g1 = (h0 + a.qpk - 1) / a.hpg;
-    const int len = max(seq_len(a, b), 0);
-    uint32_t on = mrow[g0];
-    for (int g = g0 + 1; g <= g1; ++g) on |= mrow[g];
-    const int n = on ? (len + kU - 1) / kU : 0;
-    s_pre[p] = n;
-    sum += (uint64_t)(n > 0) << 40 | (uint32_t)n;
-  }
-  uint64_t x = sum;  // inclusive scan over the wave, then over the waves
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const uint64_t y = __shfl_up((unsigned long long)x, d);
-    if (lane >= d) x += y;
-  }
-  if (lane == kWave - 1) s_sum[w] = x;
-  __syncthreads();
-  uint64_t run = x - sum, all = 0;
-#pragma unroll
-  for (int i = 0; i < kDT / kWave; ++i) {
-    if (i < w) run += s_sum[i];
-    all += s_sum[i];
-  }
-  const int units = (int)(all & kUnitBits), q = max((units + a.waves - 1) / a.waves, kMinUnits);
-  for (int p = p0; p < p1; ++p) {
-    const int n = (int)s_pre[p], u = (int)(run & kUnitBits), rank = (int)(run >> 40);
-    s_pre[p] = run;
-    if (blockIdx.x == 0) {
-      a.table[2 * p] = u / q + rank;
-      a.table[2 * p + 1] = n > 0 ? (u + n - 1) / q - u / q + 1 : 0;
-    }
-    run += (uint64_t)(n > 0) << 40 | (uint32_t)n;
-  }
-  if (tid == 0) {
-    s_pre[P] = all;
-    s_sum[kDT / kWave] = (uint64_t)q;
-  }
-  __syncthreads();
-}
+constexpr int kMinUnits = 4;  // 64 keys: the shortest run of the balanced split
 
 // HMAX: the most query heads per KV head this instance serves (qpk <= HMAX);
 // BAL: balanced split, else equal chunks.
@@ -139,13 +67,13 @@ __global__ __launch_bounds__(kDT, HMAX <= 8 ? 2 : 1) void wide_attn_decode(AttnD
   __shared__ __attribute__((aligned(16))) float s_p[4][kU][16];  // per wave: p[key][head]
   __shared__ __attribute__((aligned(16))) float s_al[4][16];     // per wave: rescale per head
   extern __shared__ uint64_t s_pre[];  // balanced: units and active pairs before each pair
-  __shared__ uint64_t s_sum[kDT / kWave + 1];
+  __shared__ uint64_t s_sum[kSplitThreads / kWave + 1];
   const int w = wave_id(), lane = lane_id();
   int p, slot, j_begin, j_end, u_end = 0, wave = 0, rank = 0;
   auto pre = [&](int i) { return (int)(s_pre[i] & kUnitBits); };
   if constexpr (BAL) {
-    list_units(a, s_pre, s_sum);
-    const int P = a.B * a.n_kv, q = __builtin_amdgcn_readfirstlane((int)s_sum[kDT / kWave]);
+    list_units<kU, kMinUnits>(a, s_pre, s_sum);
+    const int P = a.B * a.n_kv, q = __builtin_amdgcn_readfirstlane((int)s_sum[kSplitThreads / kWave]);
     const int units = pre(P), nwg = (int)(((int64_t)units + 4 * q - 1) / (4 * q));
     if ((int)blockIdx.x >= nwg) return;
     // Workgroups with work take their waves' runs in order, neighbours on
@@ -160,17 +88,7 @@ __global__ __launch_bounds__(kDT, HMAX <= 8 ? 2 : 1) void wide_attn_decode(AttnD
     const int64_t u0 = (int64_t)wave * q;
     if (u0 >= units) return;
     u_end = (int)min(u0 + q, (int64_t)units);
-    // the pair of unit u0, the last one with at most u0 units before it: 64
-    // candidates per step, one per lane
-    int lo = 0, n = P;
-    while (n > 1) {
-      const int st = (n + kWave - 1) / kWave, i = lo + lane * st;
-      const uint64_t le = __ballot(lane * st < n && pre(min(i, P)) <= (int)u0);
-      const int k = 63 - __builtin_clzll(le);  // (lane 0's candidate always qualifies)
-      n = min(st, n - k * st);
-      lo += k * st;
-    }
-    p = __builtin_amdgcn_readfirstlane(lo);
+    p = pair_of_unit(s_pre, P, (int)u0);
     rank = __builtin_amdgcn_readfirstlane((int)(s_pre[p] >> 40));
     j_begin = (int)(u0 - pre(p)) * kU;
   } else {
@@ -462,10 +380,6 @@ hipError_t launch_attention_decode(AttnDecArgs a, hipStream_t s) {
 #undef WIDE_DEC
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return launch_attention_decode_merge(a, s);
-}
-
-hipError_t launch_attention_decode_merge(const AttnDecArgs& a, hipStream_t s) {
   const int heads = a.B * a.n_q;
   const bool wide_merge = a.n_chunks > (heads <= 1024 ? 4 : 8) &&
                           (heads <= 2048 || (a.table && a.waves >= 4 * a.B * a.n_kv));

@@ -292,8 +292,6 @@ int attn_decode_chunk(int B, int n_kv, int L);
 constexpr int kAttnDecMaxPairs = 2016, kAttnDecWaves = 2048;
 int attn_decode_waves(int64_t B, int n_kv, int L);  // 0: no balanced split for this shape
 hipError_t launch_attention_decode(AttnDecArgs a, hipStream_t s);
-// The second kernel: one pair's partials to o (also run over the 4-bit cache's).
-hipError_t launch_attention_decode_merge(const AttnDecArgs& a, hipStream_t s);
 
 // ---- 4-bit KV cache (kv_quant.hip, attention_decode_kvq.hip)
 struct KvqArgs {
@@ -308,8 +306,13 @@ struct KvqArgs {
   int head_major;
 };
 hipError_t launch_kv_quant(const KvqArgs& a, bool f32, bool read, hipStream_t s);
-// a.k and a.v are the 4-bit caches; quant_groups per row: 1, 2 or 4
-int attn_decode_kvq_chunk(int64_t B, int n_kv, int L);
+// Decode attention; a.k and a.v are the 4-bit caches, quant_groups per row 1, 2
+// or 4.  a.table and a.part (of the waves that share the work) as for the bf16
+// cache's balanced split; no table: one workgroup per pair.
+constexpr int kKvqMaxPairs = 8000;  // listed in LDS: two workgroups of a CU hold 64 KB each
+constexpr int kKvqMinTiles = 2;     // 64 keys: the shortest run of a wave
+int attn_decode_kvq_waves(int64_t B, int n_kv, int L);
+size_t attn_decode_kvq_part_floats(int64_t B, int n_kv, int qpk, int waves);
 hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStream_t s);
 
 hipError_t launch_gemv_n(const GVNArgs& a, bool swiglu, hipStream_t s);
