@@ -2,29 +2,36 @@
 //
 // The mathematics of attention_decode.hip with K and V read as codes: a row
 // stands for low_g + s_g c_d in the dimensions d of group g, so
-//   score  = sum_g s_g ((16 + c) . q)_g + (low_g - 16 s_g) sum(q)_g,
+//   score  = sum_g s_g (c . q)_g + low_g sum(q)_g,
 //   output = sum_j p_j s_jg (16 + c_jd) + p_j (low_jg - 16 s_jg).
-// A bf16 with exponent 2^4 and the code in its top four mantissa bits is 16 + c
-// exactly, so one shift and one and-or turn a 32-bit word of codes into two
-// MFMA operands; nothing is dequantised.
+// Nothing is dequantised.
 //
 // A wave takes tiles of 32 keys of one (sequence, KV head) pair, straight into
-// registers, every query head of the KV head packed in the MFMA's 16 columns.
-// Short contexts: one workgroup per pair, its waves take tiles in turn, meet in
-// LDS and store o.  Longer ones: every wave takes an equal run of the active
-// pairs' tiles (decode_split.h) and leaves a (maximum, sum, unnormalised o) per
-// pair it meets; a second kernel joins them.  Per tile, on
-// v_mfma_f32_16x16x32_bf16 unless noted:
-//   scores  D_g[key][head] = (16 + c) q, a 32-wide group of dimensions each;
-//           the scales as [key][head] in the same registers come from a
-//           16x16x16 MFMA of the rows' (scale, low) with a one-hot operand, the
-//           low terms from one with sum(q) (in three bf16 parts: 24 bits);
+// registers, and the KV head's query heads in sets of four.  Short contexts:
+// one workgroup per pair, its waves take tiles in turn, meet in LDS and store
+// o.  Longer ones: every wave takes an equal run of the active pairs' tiles
+// (decode_split.h) and leaves a (maximum, sum, unnormalised o) per pair it
+// meets; a second kernel joins them.
+//
+// The MFMAs' sixteen columns (rows, for P.V) are (head h of the set, 32-wide
+// group g of the dimensions), 4 h + g, so that a scale multiplies a value of
+// one group where it stands and no lane repeats another's work.  Per tile:
+//   scores  D[key][h, g] = c . q over group g, one 16x16x128 fp8 MFMA per 16
+//           keys: a byte 0000cccc is the e4m3 number c 2^-9, so a mask (and a
+//           shift) makes operands of the codes; q as two e4m3 terms (its eight
+//           bits, both scaled by a power of two per head that the MFMA's block
+//           scale takes back) with zeros outside group g.  The scales s_g[key]
+//           come in the same layout from a 16x16x16 bf16 MFMA of the rows'
+//           (scale, low) with a one-hot operand, low_g sum(q)_g from one with
+//           sum(q) in three bf16 parts (24 bits).  The four groups' sums meet
+//           within the lanes of a quad, which share out the four keys of each;
 //   softmax online per head, fp32.  The maximum moves only when a score passes
 //           it by 8 (in the exponent), so p <= 2^8, and most tiles rescale
 //           nothing;
-//   P.V     p s_g [head][key], straight from the scores' registers, in two
-//           bf16 parts (2^-16 relative; up to 8 heads the second part sits in
-//           the columns 8..15), times 16 + c; 8 columns of words a lane.
+//   P.V     p s_g [h, g][key] in two bf16 parts (2^-16 relative), two MFMAs for
+//           each nibble of the words; 16 + c is a bf16 with exponent 2^4 and the
+//           code in its top mantissa bits: a shift and an and-or make two.  Row
+//           (h, g) holds dimensions of group g in nibbles g and g + 4 only.
 // The low terms of P.V are fp32 sums per (head, group) beside it.
 #include <algorithm>
 
@@ -69,32 +76,48 @@ __device__ __forceinline__ u32x2 load_meta(bufview_t v, uint32_t off, uint32_t s
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(v, (int)off, (int)soff, 0));
 }
 
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// 16x16x128 MFMA of e4m3 bytes.  Lane l holds A[row = l%16] and B[col = l%16],
+// 32 bytes each of k block l/16 (the same order on both sides); the result is
+// laid out as mfma16's.  Codes c stand for c 2^-9 (undone by A's scale);
+// b_scale is the exponent byte of this lane's column.
+__device__ __forceinline__ f32x4 mfma_codes(i32x8 a, i32x8 b, f32x4 c, int b_scale) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 127 + 9, 0, b_scale);
+}
+
+// Lane l ^ D of each quad; lane R of each quad.
+template <int D>
+__device__ __forceinline__ float quad_xor(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), D == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true));
+}
+template <int R>
+__device__ __forceinline__ float quad_bcast(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), R * 0x55, 0xF, 0xF, true));
+}
+
 template <int NG>
 struct Tile {
-  u32x4 kc[2];   // lane: key 16t + l%16, words 4 (l/16) .. +4
-  u32x2 km[2];   // lane: (scale, low) of that key
+  u32x4 kc[2];        // lane: key 16t + l%16, words 4 (l/16) .. +4
+  u32x2 km[2];        // lane: (scale, low) of that key
   uint32_t vc[2][4];  // lane: key 16t + 4 (l/16) + r, word l%16
-  u32x2 vm[2];   // as km
+  u32x2 vm[2];        // as km
 };
 
-// W16: 9..16 query heads per KV head (both parts of p s in MFMAs of their own).
-// Keys j, j + 1, .. of tiles at j, j + step, .. below j1 (at least one), for
-// the heads `act` of pair (b, hkv).  emit(head, maximum, sum) and
-// store(head, dim, o) receive the unnormalised result.
-template <int NG, bool W16, class Emit, class Store>
-__device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, uint32_t act, int j, int step, int j1,
+// NS sets of four query heads (the KV head has at most 4 NS).  Tiles at keys j,
+// j + step, .. below j1 (at least one), for the heads act() of pair (b, hkv).
+// emit(head, maximum, sum) and store(head, dim, o[dim], o[dim + 1]) receive the
+// unnormalised result.
+template <int NG, int NS, class Act, class Emit, class Store>
+__device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, Act act_of, int j, int step, int j1,
                                        Emit emit, Store store) {
   constexpr int R = 64 + 4 * NG;       // bytes of a cache row
-  constexpr int GQ = 4 / NG;           // 32-wide groups per quantisation group
   const int lane = lane_id(), l16 = lane & 15, g4 = lane >> 4;
-  const int hc = W16 ? l16 : l16 & 7;  // this lane's head column
-  u32x4 qf[4];
-  {
-    const bool on = hc < a.qpk && ((act >> hc) & 1u);
-    const uint16_t* qp = a.q + ((int64_t)b * a.n_q + hkv * a.qpk + (on ? hc : 0)) * 128 + 8 * g4;
+  const int g = l16 & 3, hl = l16 >> 2;  // this lane's column: group, head of the set
+  u32x4 qr[NS];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) qf[g] = on ? ldg16(qp + 32 * g) : u32x4{0, 0, 0, 0};
-  }
+  for (int s = 0; s < NS; ++s)
+    qr[s] = ldg16(a.q + ((int64_t)b * a.n_q + hkv * a.qpk + min(4 * s + hl, a.qpk - 1)) * 128 + 32 * g + 8 * g4);
   // ---- loads: a view per tile of the rows up to j1; rows past them read zeros
   const uint32_t ld = a.head_major ? R : (uint32_t)a.n_kv * R;
   const int64_t base = a.head_major ? ((int64_t)b * a.n_kv + hkv) * a.L * R
@@ -121,196 +144,198 @@ __device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, uin
       T.vm[t] = load_meta<NG>(vv, m_off, 16 * t * ld);
     }
   };
-
   Tile<NG> t0, t1;
   load(j, t0);
   load(j + step, t1);
 
   // ---- operands that stay
-  float sq[4];                         // sum of q over each 32-wide group
-  {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      float s = 0.0f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) s += __uint_as_float(qf[g][e] << 16) + __uint_as_float(qf[g][e] & 0xffff0000u);
-      s += __shfl_xor(s, 16);
-      sq[g] = s + __shfl_xor(s, 32);
-    }
-    if constexpr (NG == 2) {
-      sq[0] += sq[1];
-      sq[1] = sq[2] + sq[3];
-    } else if constexpr (NG == 1) {
-      sq[0] = (sq[0] + sq[1]) + (sq[2] + sq[3]);
-    }
-  }
-  // part i of x in bf16: x = part 0 + part 1 + part 2 (8 bits each)
-  auto part = [](float x, int i) {
-    float h = 0.0f;
-    for (int k = 0; k <= i; ++k) {
-      x -= h;
-      h = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-    }
-    return h;
-  };
-  u32x2 b_low[2], b_s[NG], b_lo[NG];  // B operands: sum(q) terms, one-hot scale, one-hot low - 16 scale
-  {
-    auto pk = [](float x, float y) { return __float_as_uint(x) >> 16 | (__float_as_uint(y) & 0xffff0000u); };
+  const uint32_t act = act_of();
+  i32x8 q_hi[NS], q_lo[NS];            // q 2^e in two e4m3 terms, the second times 2^5
+  int q_sc[NS];                        // the exponent byte that undoes e
+  u32x2 b_low[NS][2];                  // sum(q) of (h, g) in three parts, at the place of low_g
+  auto pk = [](float x, float y) { return __float_as_uint(x) >> 16 | (__float_as_uint(y) & 0xffff0000u); };
+  // the one-hot operands: the place of s_g, and of low_g with -16 at s_g
+  constexpr int GQ = 4 / NG;
+  const int slot = g / GQ;             // the quantisation group of this column
+  auto place = [&](float s, float low) {  // (scale place of this column's group) = s, (low place) = low
     if constexpr (NG == 4) {
-      const float f = g4 & 1 ? 1.0f : -16.0f;
-      const int pt = g4 >> 1;
-      b_low[0] = u32x2{pk(f * part(sq[0], pt), f * part(sq[1], pt)), pk(f * part(sq[2], pt), f * part(sq[3], pt))};
-      const float f2 = g4 < 2 ? f : 0.0f;
-      b_low[1] = u32x2{pk(f2 * part(sq[0], 2), f2 * part(sq[1], 2)), pk(f2 * part(sq[2], 2), f2 * part(sq[3], 2))};
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const uint32_t sh = g & 1 ? 16 : 0;
-        const uint32_t one = g4 == 0 ? 0x3f80u << sh : 0u;
-        const uint32_t lo = g4 == 0 ? 0xc180u << sh : g4 == 1 ? 0x3f80u << sh : 0u;
-        b_s[g] = g < 2 ? u32x2{one, 0u} : u32x2{0u, one};
-        b_lo[g] = g < 2 ? u32x2{lo, 0u} : u32x2{0u, lo};
-      }
+      const float x = g4 & 1 ? low : s;
+      return u32x2{pk(slot == 0 ? x : 0.0f, slot == 1 ? x : 0.0f), pk(slot == 2 ? x : 0.0f, slot == 3 ? x : 0.0f)};
+    } else if constexpr (NG == 2) {
+      return u32x2{pk(slot == 0 ? s : 0.0f, slot == 1 ? s : 0.0f), pk(slot == 0 ? low : 0.0f, slot == 1 ? low : 0.0f)};
     } else {
-      const int pt = min(g4, 2);
-      const float f = g4 < 3 ? 1.0f : 0.0f;
-      if constexpr (NG == 2) {
-        const float x = f * part(sq[0], pt), y = f * part(sq[1], pt);
-        b_low[0] = u32x2{pk(-16.0f * x, -16.0f * y), pk(x, y)};
+      return u32x2{pk(s, low), 0u};
+    }
+  };
+  const float first = g4 < (NG == 4 ? 2 : 1) ? 1.0f : 0.0f;  // (each place counts once)
+  const u32x2 b_s = place(first, 0.0f), b_lo = place(-16.0f * first, first);
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          const uint32_t sh = g & 1 ? 16 : 0;
-          b_s[g] = u32x2{g4 == 0 ? 0x3f80u << sh : 0u, 0u};
-          b_lo[g] = u32x2{g4 == 0 ? 0xc180u << sh : 0u, g4 == 0 ? 0x3f80u << sh : 0u};
-        }
-      } else {
-        const float x = f * part(sq[0], pt);
-        b_low[0] = u32x2{pk(-16.0f * x, x), 0u};
-        b_s[0] = u32x2{g4 == 0 ? 0x3f80u : 0u, 0u};
-        b_lo[0] = u32x2{g4 == 0 ? 0x3f80c180u : 0u, 0u};
-      }
+  for (int s = 0; s < NS; ++s) {
+    const bool on = 4 * s + hl < a.qpk && ((act >> (4 * s + hl)) & 1u);
+    float x[8], mx = 0.0f, sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t w = on ? qr[s][e] : 0u;
+      x[2 * e] = __uint_as_float(w << 16);
+      x[2 * e + 1] = __uint_as_float(w & 0xffff0000u);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      mx = fmaxf(mx, fabsf(x[e]));
+      sum += x[e];
+    }
+    mx = fmaxf(mx, quad_xor<1>(mx));
+    mx = fmaxf(mx, quad_xor<2>(mx));
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    // max |q| 2^e in [128, 256); tiny heads: as far up as the scale byte goes
+    const int e2 = min(134 - (int)(__float_as_uint(mx) >> 23), 122);
+    q_sc[s] = 127 - e2;
+    i32x8 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float y0 = __builtin_amdgcn_ldexpf(x[2 * i], e2), y1 = __builtin_amdgcn_ldexpf(x[2 * i + 1], e2);
+      const int h = __builtin_amdgcn_cvt_pk_fp8_f32(y0, y1, 0, false);
+      const int l = __builtin_amdgcn_cvt_pk_fp8_f32(32.0f * (y0 - __builtin_amdgcn_cvt_f32_fp8(h, 0)),
+                                                    32.0f * (y1 - __builtin_amdgcn_cvt_f32_fp8(h, 1)), 0, false);
+      // nibble g of word 4 (l/16) + i: byte g / 2 of the even or the odd nibbles; nibble g + 4 two bytes on
+      const int sh = g & 2 ? 8 : 0;
+      const int hb = ((h & 0xff) | (h & 0xff00) << 8) << sh, lb = ((l & 0xff) | (l & 0xff00) << 8) << sh;
+      hi[i] = g & 1 ? 0 : hb;
+      hi[4 + i] = g & 1 ? hb : 0;
+      lo[i] = g & 1 ? 0 : lb;
+      lo[4 + i] = g & 1 ? lb : 0;
+    }
+    q_hi[s] = hi;
+    q_lo[s] = lo;
+    // sum = p0 + p1 + p2, eight bits each
+    const float p0 = __uint_as_float(__float_as_uint(sum) & 0xffff0000u), r1 = sum - p0;
+    const float p1 = __uint_as_float(__float_as_uint(r1) & 0xffff0000u), p2 = r1 - p1;
+    if constexpr (NG == 4) {
+      b_low[s][0] = place(0.0f, g4 == 1 ? p0 : p1);
+      b_low[s][1] = place(0.0f, g4 == 1 ? p2 : 0.0f);
+    } else {
+      b_low[s][0] = place(0.0f, g4 == 0 ? p0 : g4 == 1 ? p1 : g4 == 2 ? p2 : 0.0f);
     }
   }
 
   const float sc = a.scale_log2, slack = 8.0f / sc;
-  float m = -INFINITY, msc = -INFINITY, z = 0.0f;  // of head column hc: the maximum, m sc, this lane's share of the sum
-  float lo[NG];                                    // this lane's share of sum p (low - 16 s)
-  f32x4 acc[8];                                    // [head row][word l16], nibble n
+  // of head (set, hl): the maximum, m sc, this lane's share of the sum
+  float m[NS], msc[NS], z[NS];
+  float lo[NS];                        // of column (h, g): this lane's share of sum p (low - 16 s)
+  f32x4 acc[NS][8];                    // [row 4 (l/16) + group][word l16] of nibble n
 #pragma unroll
-  for (int g = 0; g < NG; ++g) lo[g] = 0.0f;
+  for (int s = 0; s < NS; ++s) {
+    m[s] = msc[s] = -INFINITY;
+    z[s] = lo[s] = 0.0f;
 #pragma unroll
-  for (int n = 0; n < 8; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int n = 0; n < 8; ++n) acc[s][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
   uint32_t sixteens = 0x41804180u;
   asm("" : "+v"(sixteens));
-  const float second = !W16 && l16 >= 8 ? 1.0f : 0.0f;
+  const bool odd = g & 1, upper = g & 2;
 
   auto process = [&](int j, const Tile<NG>& T) {
-    f32x4 S[2];
+    i32x8 A[2];
+    f32x4 ks[2], vs[2], vl[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      S[t] = mfma16k16(T.km[t], b_low[0], zero);
-      if (NG == 4) S[t] = mfma16k16(T.km[t], b_low[1], S[t]);
-      f32x4 D[NG];
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        u32x4 A;
+      for (int i = 0; i < 4; ++i) {
+        A[t][i] = (int)(T.kc[t][i] & 0x0f0f0f0fu);
+        A[t][4 + i] = (int)((T.kc[t][i] >> 4) & 0x0f0f0f0fu);
+      }
+      ks[t] = mfma16k16(T.km[t], b_s, zero);
+      vs[t] = mfma16k16(T.vm[t], b_s, zero);
+      vl[t] = mfma16k16(T.vm[t], b_lo, zero);
+    }
+    u32x4 P1[NS], P2[NS];              // p s, first and second part
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          A[i] = g == 0 ? codes<0>(T.kc[t][i], sixteens) : g == 1 ? codes<1>(T.kc[t][i], sixteens) : g == 2 ? codes<2>(T.kc[t][i], sixteens)
-                                                                                          : codes<3>(T.kc[t][i], sixteens);
-        D[g / GQ] = mfma16(A, qf[g], g % GQ == 0 ? zero : D[g / GQ]);
+    for (int s = 0; s < NS; ++s) {
+      float S[2];                      // of key 16t + 4 (l/16) + g
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f32x4 D = mfma_codes(A[t], q_hi[s], zero, q_sc[s]);
+        D = mfma_codes(A[t], q_lo[s], D, q_sc[s] - 5);
+        f32x4 x = mfma16k16(T.km[t], b_low[s][0], zero);
+        if (NG == 4) x = mfma16k16(T.km[t], b_low[s][1], x);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = fmaf(D[r], ks[t][r], x[r]);
+        const float y0 = (odd ? x[1] : x[0]) + quad_xor<1>(odd ? x[0] : x[1]);
+        const float y1 = (odd ? x[3] : x[2]) + quad_xor<1>(odd ? x[2] : x[3]);
+        S[t] = (upper ? y1 : y0) + quad_xor<2>(upper ? y0 : y1);
+      }
+      if (j + kTile > j1) {  // the last tile
+        asm volatile("");    // (a branch, not instructions in every tile)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          if (j + 16 * t + 4 * g4 + g >= j1) S[t] = -INFINITY;
+      }
+      float mx = fmaxf(S[0], S[1]);
+      if (__any(mx > m[s] + slack)) {
+        mx = fmaxf(mx, quad_xor<1>(mx));
+        mx = fmaxf(mx, quad_xor<2>(mx));
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mn = fmaxf(m[s], mx), ms = mn * sc;
+        const float al = mn == m[s] ? 1.0f : __builtin_amdgcn_exp2f(msc[s] - ms);
+        m[s] = mn;
+        msc[s] = ms;
+        z[s] *= al;
+        lo[s] *= al;
+        const float ar = __shfl(al, 4 * g4);  // of the head this lane's rows belong to
+#pragma unroll
+        for (int n = 0; n < 8; ++n) acc[s][n][n & 3] *= ar;
       }
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        const f32x4 s = mfma16k16(T.km[t], b_s[g], zero);
+      for (int t = 0; t < 2; ++t) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(S[t], sc, -msc[s]));
+        z[s] += p;
+        float x[4], y[4];
+        x[0] = quad_bcast<0>(p) * vs[t][0];
+        x[1] = quad_bcast<1>(p) * vs[t][1];
+        x[2] = quad_bcast<2>(p) * vs[t][2];
+        x[3] = quad_bcast<3>(p) * vs[t][3];
+        lo[s] = fmaf(quad_bcast<0>(p), vl[t][0], lo[s]);
+        lo[s] = fmaf(quad_bcast<1>(p), vl[t][1], lo[s]);
+        lo[s] = fmaf(quad_bcast<2>(p), vl[t][2], lo[s]);
+        lo[s] = fmaf(quad_bcast<3>(p), vl[t][3], lo[s]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][r] = fmaf(D[g][r], s[r], S[t][r]);
+        for (int r = 0; r < 4; ++r) y[r] = x[r] - __uint_as_float(__float_as_uint(x[r]) & 0xffff0000u);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          P1[s][2 * t + h] = __builtin_amdgcn_perm(__float_as_uint(x[2 * h + 1]), __float_as_uint(x[2 * h]), 0x07060302u);
+          P2[s][2 * t + h] = pack_bf16x2_hw(y[2 * h], y[2 * h + 1]);
+        }
       }
     }
-    if (j + kTile > j1) {  // the last tile
-      asm volatile("");    // (a branch, not sixteen instructions in every tile)
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (j + 16 * t + 4 * g4 + r >= j1) S[t][r] = -INFINITY;
-    }
-    float mx = fmaxf(fmaxf(fmaxf(S[0][0], S[0][1]), fmaxf(S[0][2], S[0][3])),
-                     fmaxf(fmaxf(S[1][0], S[1][1]), fmaxf(S[1][2], S[1][3])));
-    if (__any(mx > m + slack)) {
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float mn = fmaxf(m, mx), ms = mn * sc;
-      const float al = mn == m ? 1.0f : __builtin_amdgcn_exp2f(msc - ms);
-      m = mn;
-      msc = ms;
-      z *= al;
-#pragma unroll
-      for (int g = 0; g < NG; ++g) lo[g] *= al;
-      f32x4 ar;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) ar[r] = __shfl(al, 4 * g4 + r);
-#pragma unroll
-      for (int n = 0; n < 8; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[n][r] *= ar[r];
-    }
-    float P[2][4];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        P[t][r] = __builtin_amdgcn_exp2f(fmaf(S[t][r], sc, -msc));
-        z += P[t][r];
-      }
     // pairs of keys, nibbles 0..3 and 4..7 of the words
-    uint32_t vl[4], vh[4];
+    uint32_t wl[4], wh[4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        vl[2 * t + h] = __builtin_amdgcn_perm(T.vc[t][2 * h + 1], T.vc[t][2 * h], 0x05040100u);
-        vh[2 * t + h] = __builtin_amdgcn_perm(T.vc[t][2 * h + 1], T.vc[t][2 * h], 0x07060302u);
+        wl[2 * t + h] = __builtin_amdgcn_perm(T.vc[t][2 * h + 1], T.vc[t][2 * h], 0x05040100u);
+        wh[2 * t + h] = __builtin_amdgcn_perm(T.vc[t][2 * h + 1], T.vc[t][2 * h], 0x07060302u);
       }
-    u32x4 A, A2;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      if (g % GQ == 0) {
-        const int G = g / GQ;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const f32x4 s = mfma16k16(T.vm[t], b_s[G], zero), l = mfma16k16(T.vm[t], b_lo[G], zero);
-          float x[4], y[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            lo[G] = fmaf(P[t][r], l[r], lo[G]);
-            x[r] = P[t][r] * s[r];
-            const float hi = __uint_as_float(__float_as_uint(x[r]) & 0xffff0000u);
-            if constexpr (W16) {
-              y[r] = x[r] - hi;
-              x[r] = hi;
-            } else {
-              x[r] = fmaf(second, x[r], -hi);  // -hi, or x - hi
-            }
-          }
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            A[2 * t + h] = pack_bf16x2_hw(x[2 * h], x[2 * h + 1]);
-            if constexpr (W16) A2[2 * t + h] = pack_bf16x2_hw(y[2 * h], y[2 * h + 1]);
-          }
-        }
-      }
-      u32x4 B0, B1;
+    for (int n = 0; n < 8; ++n) {
+      u32x4 B;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        B0[i] = g == 0 ? codes<0>(vl[i], sixteens) : g == 1 ? codes<1>(vl[i], sixteens) : g == 2 ? codes<2>(vl[i], sixteens) : codes<3>(vl[i], sixteens);
-        B1[i] = g == 0 ? codes<0>(vh[i], sixteens) : g == 1 ? codes<1>(vh[i], sixteens) : g == 2 ? codes<2>(vh[i], sixteens) : codes<3>(vh[i], sixteens);
+        const uint32_t w = n < 4 ? wl[i] : wh[i];
+        B[i] = (n & 3) == 0   ? codes<0>(w, sixteens)
+               : (n & 3) == 1 ? codes<1>(w, sixteens)
+               : (n & 3) == 2 ? codes<2>(w, sixteens)
+                              : codes<3>(w, sixteens);
       }
-      acc[g] = mfma16(A, B0, acc[g]);
-      acc[4 + g] = mfma16(A, B1, acc[4 + g]);
-      if constexpr (W16) {
-        acc[g] = mfma16(A2, B0, acc[g]);
-        acc[4 + g] = mfma16(A2, B1, acc[4 + g]);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        acc[s][n] = mfma16(P1[s], B, acc[s][n]);
+        acc[s][n] = mfma16(P2[s], B, acc[s][n]);
       }
     }
   };
@@ -324,33 +349,21 @@ __device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, uin
   }
   if (j < j1) process(j, t0);
 
-  z += __shfl_xor(z, 16);
-  z += __shfl_xor(z, 32);
 #pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    lo[g] += __shfl_xor(lo[g], 16);
-    lo[g] += __shfl_xor(lo[g], 32);
-  }
-  if (g4 == 0 && l16 < a.qpk) emit(l16, msc, z);
-  if constexpr (W16) {
+  for (int s = 0; s < NS; ++s) {
+    float zs = z[s], ls = lo[s];
+    zs += quad_xor<1>(zs);
+    zs += quad_xor<2>(zs);
+    zs += __shfl_xor(zs, 16);
+    zs += __shfl_xor(zs, 32);
+    ls += __shfl_xor(ls, 16);
+    ls += __shfl_xor(ls, 32);
+    if (g4 == 0 && g == 0 && 4 * s + hl < a.qpk) emit(4 * s + hl, msc[s], zs);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int n = 0; n < 8; ++n) store(4 * g4 + r, 32 * (n & 3) + 2 * l16 + (n >> 2),
-                                        acc[n][r] + __shfl(lo[(n & 3) / GQ], 4 * g4 + r));
-  } else {
-    // the two parts of p s (rows h and 8 + h; the first with its sign turned),
-    // nibbles g and g + 4 in the two halves of the wave
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[g][r]), __float_as_uint(acc[g + 4][r]),
-                                                         false, false);
-        const int h = 4 * (g4 & 1) + r;
-        store(h, 32 * g + 2 * l16 + (g4 >> 1),
-              __uint_as_float(sw[1]) - __uint_as_float(sw[0]) + __shfl(lo[g / GQ], h));
-      }
+    for (int n = 0; n < 4; ++n) {
+      const float l = __shfl(ls, 4 * g4 + n);
+      store(4 * s + g4, 32 * n + 2 * l16, acc[s][n][n] + l, acc[s][4 + n][n] + l);
+    }
   }
 }
 
@@ -361,11 +374,10 @@ __device__ __forceinline__ uint32_t active_mask(const AttnDecArgs& a, int b, int
   return (uint32_t)__ballot(on != 0) & ((1u << a.qpk) - 1);
 }
 
-// One workgroup per pair.
-template <int NG, bool W16, int NW>
-__global__ __launch_bounds__(NW * 64, 2) void wide_attn_decode_kvq(AttnDecArgs a) {
-  constexpr int H = W16 ? 16 : 8;
-  __shared__ float s_o[NW][H][128 + 4];
+// One workgroup of NW waves per pair.
+template <int NG, int NS, int NW>
+__global__ __launch_bounds__(NW * 64, NS < 4 ? 2 : 1) void wide_attn_decode_kvq(AttnDecArgs a) {
+  __shared__ float s_o[NW][4 * NS][128 + 4];
   __shared__ float s_m[NW][16], s_z[NW][16];
   const int w = wave_id(), p = xcd_remap(blockIdx.x, gridDim.x), b = p / a.n_kv, hkv = p - b * a.n_kv;
   const int len = seq_len(a, b);
@@ -376,13 +388,13 @@ __global__ __launch_bounds__(NW * 64, 2) void wide_attn_decode_kvq(AttnDecArgs a
     return;
   }
   if (w * kTile < len)
-    attend<NG, W16>(
-        a, b, hkv, act, w * kTile, NW * kTile, len,
+    attend<NG, NS>(
+        a, b, hkv, [&] { return act; }, w * kTile, NW * kTile, len,
         [&](int h, float m, float z) {
           s_m[w][h] = m;
           s_z[w][h] = z;
         },
-        [&](int h, int d, float x) { s_o[w][h][d] = x; });
+        [&](int h, int d, float x, float y) { *reinterpret_cast<float2*>(&s_o[w][h][d]) = float2{x, y}; });
   __syncthreads();
   const int nw = min(NW, (len + kTile - 1) / kTile);  // waves that had a tile
   for (int i = threadIdx.x; i < a.qpk * 64; i += NW * 64) {
@@ -404,8 +416,8 @@ __global__ __launch_bounds__(NW * 64, 2) void wide_attn_decode_kvq(AttnDecArgs a
 constexpr int kPart = 4 + 128;  // floats of a partial: maximum, sum, (two unused), o
 
 // Equal runs of tiles a wave.
-template <int NG, bool W16>
-__global__ __launch_bounds__(kSplitThreads, 2) void wide_attn_decode_kvq_runs(AttnDecArgs a) {
+template <int NG, int NS>
+__global__ __launch_bounds__(kSplitThreads, NS < 4 ? 2 : 1) void wide_attn_decode_kvq_runs(AttnDecArgs a) {
   extern __shared__ uint64_t s_pre[];  // tiles and active pairs before each pair
   __shared__ uint64_t s_sum[kSplitThreads / kWave + 1];
   list_units<kTile, kKvqMinTiles>(a, s_pre, s_sum);
@@ -423,16 +435,15 @@ __global__ __launch_bounds__(kSplitThreads, 2) void wide_attn_decode_kvq_runs(At
     p = __builtin_amdgcn_readfirstlane(p);
     const int b = p / a.n_kv, hkv = p - b * a.n_kv;
     const int j1 = __builtin_amdgcn_readfirstlane((int)min((int64_t)seq_len(a, b), (int64_t)(u_end - pre(p)) * kTile));
-    const uint32_t act = active_mask(a, b, hkv);
     float* part = a.part + (int64_t)(wave + rank) * a.qpk * kPart;
-    attend<NG, W16>(
-        a, b, hkv, act, j, kTile, j1,
+    attend<NG, NS>(
+        a, b, hkv, [&] { return active_mask(a, b, hkv); }, j, kTile, j1,
         [&](int h, float m, float z) {
           part[h * kPart] = m;
           part[h * kPart + 1] = z;
         },
-        [&](int h, int d, float x) {
-          if (h < a.qpk) part[h * kPart + 4 + d] = x;
+        [&](int h, int d, float x, float y) {
+          if (h < a.qpk) *reinterpret_cast<float2*>(part + h * kPart + 4 + d) = float2{x, y};
         });
     if (u_end <= pre(p + 1)) break;
   }
@@ -534,25 +545,26 @@ size_t attn_decode_kvq_part_floats(int64_t B, int n_kv, int qpk, int waves) {
 
 hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStream_t s) {
   if (a.B == 0) return hipSuccess;
-  constexpr int NW = 8;
   const int pairs = a.B * a.n_kv, lds = (pairs + 1) * (int)sizeof(uint64_t);
-#define WIDE_DEC4(NG, W16)                                                                                       \
-  do {                                                                                                           \
-    if (a.table)                                                                                                 \
-      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_runs<NG, W16>), dim3(a.waves / 4),         \
-                        dim3(kSplitThreads), lds, s, a);                                                         \
-    else                                                                                                         \
-      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq<NG, W16, NW>), dim3(pairs), dim3(NW * 64), \
-                        0, s, a);                                                                                \
+#define WIDE_DEC4(NG, NS)                                                                                    \
+  do {                                                                                                       \
+    constexpr int NW = NS < 4 ? 8 : 4;                                                                       \
+    if (a.table)                                                                                             \
+      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_runs<NG, NS>), dim3(a.waves / 4),      \
+                        dim3(kSplitThreads), lds, s, a);                                                     \
+    else                                                                                                     \
+      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq<NG, NS, NW>), dim3(pairs), dim3(NW * 64), \
+                        0, s, a);                                                                            \
   } while (0)
-#define WIDE_DEC4_NG(W16)                        \
-  do {                                           \
-    if (quant_groups == 4) WIDE_DEC4(4, W16);    \
-    else if (quant_groups == 2) WIDE_DEC4(2, W16); \
-    else WIDE_DEC4(1, W16);                      \
+#define WIDE_DEC4_NG(NS)                        \
+  do {                                          \
+    if (quant_groups == 4) WIDE_DEC4(4, NS);    \
+    else if (quant_groups == 2) WIDE_DEC4(2, NS); \
+    else WIDE_DEC4(1, NS);                      \
   } while (0)
-  if (a.qpk > 8) WIDE_DEC4_NG(true);
-  else WIDE_DEC4_NG(false);
+  if (a.qpk <= 4) WIDE_DEC4_NG(1);
+  else if (a.qpk <= 8) WIDE_DEC4_NG(2);
+  else WIDE_DEC4_NG(4);
 #undef WIDE_DEC4_NG
 #undef WIDE_DEC4
   const hipError_t e = hipGetLastError();
