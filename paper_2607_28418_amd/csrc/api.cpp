@@ -1435,7 +1435,7 @@ struct KvqWS {
 size_t carve_attention_decode_kvq(Carve& c, int64_t B, int L, int nq, int nkv, KvqWS& w) {
   if (B == 0) return 0;
   w.waves = wide::attn_decode_kvq_waves(B, nkv, L);
-  w.table = c.take<int32_t>((size_t)B * nkv * 2);
+  w.table = c.take<int32_t>((size_t)B * nkv * 4);
   if (w.waves) w.part = c.take<float>(wide::attn_decode_kvq_part_floats(B, nkv, nq / nkv, w.waves));
   else w.table = nullptr;
   return c.off;

@@ -61,8 +61,8 @@ __device__ __forceinline__ f32x4 mfma16k16(u32x2 a, u32x2 b, f32x4 c) {
 // is two instructions.
 template <int N>
 __device__ __forceinline__ uint32_t codes(uint32_t w, uint32_t sixteens) {
-  const uint32_t x = N == 0 ? w << 3 : w >> (4 * N - 3);
-  return (x & 0x00780078u) | sixteens;
+  constexpr int S = 4 * N - 3;  // bits the nibble moves down
+  return ((S < 0 ? w << (S < 0 ? -S : 0) : w >> (S < 0 ? 0 : S)) & 0x00780078u) | sixteens;
 }
 
 // The (scale, low) words of a row as a 16x16x16 operand.  NG = 4: lanes with an
@@ -449,6 +449,144 @@ __global__ __launch_bounds__(kSplitThreads, NS < 4 ? 2 : 1) void wide_attn_decod
   }
 }
 
+// Token-major caches.  A position's rows of all KV heads lie together, a row ends
+// inside a cache line, and the next head's begins there: the waves that read the
+// same positions have to run together on one XCD, or every line comes from memory
+// once per head that touches it (32 x 8192 keys, 8 KV heads: 122 us with runs in
+// pair order, 98 here; ragged 71 and 54).  What is left over a head-major cache
+// (69) is the L1's: it holds 64 requests of a line each, and a row of 80 bytes
+// takes 1.6 of them.  So the work is cut sequence by sequence: each of its A active KV heads
+// into r = ceil(tiles / q) equal chunks, waves in (sequence, chunk, head) order,
+// neighbouring workgroups on one XCD; q is the least number of tiles for which
+// all of it fits the resident waves.  One partial a wave, in slot `wave`.
+struct SeqSplit {
+  uint32_t act;   // active KV heads
+  int first;      // waves before the sequence
+};
+template <int NG, int NS>
+__global__ __launch_bounds__(kSplitThreads, NS < 4 ? 2 : 1) void wide_attn_decode_kvq_seqs(AttnDecArgs a) {
+  extern __shared__ SeqSplit s_seq[];  // B + 1
+  __shared__ int s_cnt[kSplitThreads / kWave][kWave];
+  __shared__ int64_t s_red[kSplitThreads / kWave][2];
+  const int tid = threadIdx.x, w = wave_id(), lane = lane_id(), P = a.B * a.n_kv;
+  auto tiles = [&](int b) { return (max(seq_len(a, b), 0) + kTile - 1) / kTile; };
+  for (int b = tid; b <= a.B; b += kSplitThreads) s_seq[b].act = 0;
+  __syncthreads();
+  for (int p = tid; p < P; p += kSplitThreads) {
+    const int b = p / a.n_kv, hkv = p - b * a.n_kv, h0 = hkv * a.qpk;
+    const uint8_t* mrow = a.mask + (int64_t)b * a.ng;
+    const int g0 = h0 / a.hpg, g1 = (h0 + a.qpk - 1) / a.hpg;
+    uint32_t on = mrow[g0];
+    for (int g = g0 + 1; g <= g1; ++g) on |= mrow[g];
+    if (on) atomicOr(&s_seq[b].act, 1u << hkv);
+  }
+  __syncthreads();
+  // all tiles, and the heads that have any
+  const int per = (a.B + kSplitThreads - 1) / kSplitThreads, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
+  int64_t all = 0, heads = 0;
+  for (int b = b0; b < b1; ++b) {
+    const int n = tiles(b), A = __popc(s_seq[b].act);
+    all += (int64_t)n * A;
+    heads += n > 0 ? A : 0;
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) {
+    all += __shfl_xor((long long)all, d);
+    heads += __shfl_xor((long long)heads, d);
+  }
+  if (lane == 0) {
+    s_red[w][0] = all;
+    s_red[w][1] = heads;
+  }
+  __syncthreads();
+  all = heads = 0;
+#pragma unroll
+  for (int i = 0; i < kSplitThreads / kWave; ++i) {
+    all += s_red[i][0];
+    heads += s_red[i][1];
+  }
+  // q: sum A ceil(n / q) <= all / q + heads, so hi fits if the heads do (they are
+  // at most half of the waves: the caller's rule); 64 candidates from the mean up
+  const int lo_q = max((int)((all + a.waves - 1) / a.waves), kKvqMinTiles);
+  const int hi_q = max((int)((all + a.waves - heads - 1) / (a.waves - heads)), lo_q);
+  const int q_of = lo_q + (int)((int64_t)(hi_q - lo_q) * lane / (kWave - 1));
+  int cnt = 0;
+  for (int b = w; b < a.B; b += kSplitThreads / kWave) cnt += __popc(s_seq[b].act) * ((tiles(b) + q_of - 1) / q_of);
+  s_cnt[w][lane] = cnt;
+  __syncthreads();
+  cnt = 0;
+#pragma unroll
+  for (int i = 0; i < kSplitThreads / kWave; ++i) cnt += s_cnt[i][lane];
+  const uint64_t fits = __ballot(cnt <= a.waves);
+  const int q = __builtin_amdgcn_readlane(q_of, fits ? __builtin_ctzll(fits) : kWave - 1);
+  // waves before each sequence
+  int sum = 0;
+  for (int b = b0; b < b1; ++b) sum += __popc(s_seq[b].act) * ((tiles(b) + q - 1) / q);
+  int x = sum;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) s_cnt[w][0] = x;
+  __syncthreads();
+  int run = x - sum, total = 0;
+#pragma unroll
+  for (int i = 0; i < kSplitThreads / kWave; ++i) {
+    if (i < w) run += s_cnt[i][0];
+    total += s_cnt[i][0];
+  }
+  for (int b = b0; b < b1; ++b) {
+    s_seq[b].first = run;
+    const uint32_t act = s_seq[b].act;
+    const int A = __popc(act), r = (tiles(b) + q - 1) / q;
+    if (blockIdx.x == 0)
+      for (int h = 0; h < a.n_kv; ++h) {
+        int32_t* t = a.table + 4 * ((int64_t)b * a.n_kv + h);
+        t[0] = run + __popc(act & ((1u << h) - 1));
+        t[1] = (act >> h) & 1u ? r : 0;
+        t[2] = A;
+      }
+    run += A * r;
+  }
+  if (tid == 0) s_seq[a.B].first = total;
+  __syncthreads();
+
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int nwg = (total + 3) / 4;
+  if ((int)blockIdx.x >= nwg) return;
+  const int wave = xcd_remap(blockIdx.x, nwg) * 4 + w;
+  if (wave >= total) return;
+  int b = 0, n = a.B;  // the last sequence with at most `wave` waves before it (it has some)
+  while (n > 1) {
+    const int st = (n + kWave - 1) / kWave, i = b + lane * st;
+    const uint64_t le = __ballot(lane * st < n && s_seq[min(i, a.B)].first <= wave);
+    const int k = 63 - __builtin_clzll(le);
+    n = min(st, n - k * st);
+    b += k * st;
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  uint32_t act = __builtin_amdgcn_readfirstlane(s_seq[b].act);
+  const int at = wave - __builtin_amdgcn_readfirstlane(s_seq[b].first), A = __popc(act);
+  const int c = at / A, k = at - c * A, nt = __builtin_amdgcn_readfirstlane(tiles(b)), r = (nt + q - 1) / q;
+  for (int i = 0; i < k; ++i) act &= act - 1;
+  const int hkv = __builtin_ctz(act);
+  // chunk c of r: tiles [nt c / r, nt (c + 1) / r)
+  const int j = (int)((int64_t)nt * c / r) * kTile;
+  const int j1 = min(seq_len(a, b), (int)min((int64_t)nt * (c + 1) / r * kTile, (int64_t)a.L));
+  float* part = a.part + (int64_t)wave * a.qpk * kPart;
+  attend<NG, NS>(
+      a, b, hkv, [&] { return active_mask(a, b, hkv); }, j, kTile, __builtin_amdgcn_readfirstlane(j1),
+      [&](int h, float m, float z) {
+        part[h * kPart] = m;
+        part[h * kPart + 1] = z;
+      },
+      [&](int h, int d, float x, float y) {
+        if (h < a.qpk) *reinterpret_cast<float2*>(part + h * kPart + 4 + d) = float2{x, y};
+      });
+}
+
 // Joins a pair's partials: SL lanes of segments a head, each with four of the
 // dimensions per lane of 32.  SL = 2: a wave a head, four heads a workgroup.
 template <int SL>
@@ -460,14 +598,17 @@ __global__ __launch_bounds__(SL == 2 ? 256 : SL * 32) void wide_attn_decode_kvq_
   const int t = SL == 2 ? lane_id() : (int)threadIdx.x, dq = t & 31, sl = t >> 5;
   const int b = gh / a.n_q, h = gh - b * a.n_q, p = b * a.n_kv + h / a.qpk;
   uint32_t* out = reinterpret_cast<uint32_t*>(a.o + (int64_t)gh * 128) + 2 * dq;
-  const int nseg = a.table[2 * p + 1];
+  // (pairs in turn: two words a pair, a segment after the other; sequence by
+  // sequence: three of four words, the segments A apart)
+  const int32_t* tab = a.table + (a.by_seq ? 4 : 2) * (int64_t)p;
+  const int nseg = tab[1];
   const uint8_t on = a.mask[(int64_t)b * a.ng + h / a.hpg];
   if (!on || nseg == 0) {
     if (sl == 0) *reinterpret_cast<uint64_t*>(out) = 0;
     return;
   }
-  const int64_t ld = (int64_t)a.qpk * kPart;
-  const float* part = a.part + a.table[2 * p] * ld + (h % a.qpk) * kPart;
+  const int64_t row = (int64_t)a.qpk * kPart, ld = a.by_seq ? tab[2] * row : row;
+  const float* part = a.part + tab[0] * row + (h % a.qpk) * kPart;
   float m = -INFINITY, z = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int c = sl; c < nseg; c += 4 * SL) {
@@ -532,7 +673,7 @@ __global__ __launch_bounds__(SL == 2 ? 256 : SL * 32) void wide_attn_decode_kvq_
 
 }  // namespace
 
-constexpr int kShort = 48;  // tiles of a context that one workgroup takes alone
+constexpr int kShort = 64;  // tiles of a context that one workgroup takes alone
 
 // Waves that share the work (0: one workgroup per pair).
 int attn_decode_kvq_waves(int64_t B, int n_kv, int L) {
@@ -545,11 +686,17 @@ size_t attn_decode_kvq_part_floats(int64_t B, int n_kv, int qpk, int waves) {
 
 hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStream_t s) {
   if (a.B == 0) return hipSuccess;
+  // Sequence by sequence: the KV heads fit one word, and all of them are at most
+  // half as many as the waves.
+  a.by_seq = !a.head_major && a.n_kv > 1 && a.n_kv <= 32 && a.B * a.n_kv <= a.waves / 2;
   const int pairs = a.B * a.n_kv, lds = (pairs + 1) * (int)sizeof(uint64_t);
 #define WIDE_DEC4(NG, NS)                                                                                    \
   do {                                                                                                       \
     constexpr int NW = NS < 4 ? 8 : 4;                                                                       \
-    if (a.table)                                                                                             \
+    if (a.table && a.by_seq)                                                                                 \
+      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_seqs<NG, NS>), dim3(a.waves / 4),      \
+                        dim3(kSplitThreads), (a.B + 1) * (int)sizeof(SeqSplit), s, a);                       \
+    else if (a.table)                                                                                        \
       WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_runs<NG, NS>), dim3(a.waves / 4),      \
                         dim3(kSplitThreads), lds, s, a);                                                     \
     else                                                                                                     \

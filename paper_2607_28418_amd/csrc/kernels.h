@@ -285,6 +285,7 @@ struct AttnDecArgs {
   int waves;                // balanced split: waves sharing the work
   int B, L, n_q, n_kv, ng, hpg, qpk;
   int head_major;           // cache layout (see k)
+  int by_seq;               // (4-bit cache) the work is cut sequence by sequence: table [B * n_kv][4]
   int chunk, n_chunks;      // keys per workgroup (multiple of 64), ceil(L / chunk)
   float scale_log2;
 };
@@ -309,7 +310,7 @@ hipError_t launch_kv_quant(const KvqArgs& a, bool f32, bool read, hipStream_t s)
 // Decode attention; a.k and a.v are the 4-bit caches, quant_groups per row 1, 2
 // or 4.  a.table and a.part (of the waves that share the work) as for the bf16
 // cache's balanced split; no table: one workgroup per pair.
-constexpr int kKvqMaxPairs = 8000;  // listed in LDS: two workgroups of a CU hold 64 KB each
+constexpr int kKvqMaxPairs = 2304;  // listed in LDS beside the tiles, two workgroups a CU
 constexpr int kKvqMinTiles = 2;     // 64 keys: the shortest run of a wave
 int attn_decode_kvq_waves(int64_t B, int n_kv, int L);
 size_t attn_decode_kvq_part_floats(int64_t B, int n_kv, int qpk, int waves);
