@@ -390,53 +390,70 @@ def wide_attention_decode(q, k_cache, v_cache, mask, n_q, n_kv, head_dim, group_
 
 
 # ---- 4-bit KV cache -------------------------------------------------------------
+# (These calls take microseconds on the GPU when one token is generated, so the
+# checks below are kept to what a wrong size or device would need.)
+
+_ROW_BYTES = {}
+
 
 def wide_kv_quant_row_bytes(head_dim, quant_group) -> int:
     """Bytes of one (sequence, position, KV head) row of a 4-bit cache."""
-    n = int(lib().wide_kv_quant_row_bytes(head_dim, quant_group))
-    if n == 0:
-        raise ValueError(f"no 4-bit cache with head_dim {head_dim} and quant_group {quant_group} "
-                         "(head_dim 128; quant_group 32, 64 or 128)")
+    n = _ROW_BYTES.get((head_dim, quant_group))
+    if n is None:
+        n = int(lib().wide_kv_quant_row_bytes(head_dim, quant_group))
+        if n == 0:
+            raise ValueError(f"no 4-bit cache with head_dim {head_dim} and quant_group {quant_group} "
+                             "(head_dim 128; quant_group 32, 64 or 128)")
+        _ROW_BYTES[head_dim, quant_group] = n
     return n
 
 
-def _gpu(first, *ts):
-    """The call's tensors, all on one GPU and contiguous; returns its device."""
-    for t in (first, *ts):
-        if t is not None and (not t.is_cuda or t.device != first.device):
-            raise ValueError("tensors must be on one GPU")
-    _contig(first, *ts)
-    return first.device
+def _gpu(*ts):
+    """The call's tensors, all contiguous and on one GPU; returns its index."""
+    dev = ts[0].get_device()
+    for t in ts:
+        if t is not None:
+            if t.get_device() != dev or dev < 0:
+                raise ValueError("tensors must be on one GPU")
+            if not t.is_contiguous():
+                raise ValueError("tensors must be contiguous")
+    return dev
 
 
-class _on:
-    """The library launches on the current device: make it the tensors'."""
-    __slots__ = ("dev", "prev")
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
-    def __init__(self, dev):
-        self.dev = dev
 
-    def __enter__(self):
-        cuda = _torch().cuda
-        self.prev = cuda.current_device()
-        if self.prev != self.dev.index:
-            cuda.set_device(self.dev)
+def _raw_stream(dev):
+    """The current stream's handle on device `dev`.  torch's direct query (the
+    one its own compiled kernels use) takes 0.1 us, current_stream() 2.5."""
+    torch = _torch()
+    direct = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return direct(dev) if direct is not None else torch.cuda.current_stream(dev).cuda_stream
 
-    def __exit__(self, *exc):
-        if self.prev != self.dev.index:
-            _torch().cuda.set_device(self.prev)
+
+def _launch(name, dev, *args):
+    """Call the library on the tensors' device and its current stream."""
+    cuda = _torch().cuda
+    fn = getattr(lib(), name)
+    if cuda.current_device() == dev:
+        status = fn(*args, _raw_stream(dev))
+    else:
+        with cuda.device(dev):
+            status = fn(*args, _raw_stream(dev))
+    if status != OK:
+        _check(name, status)
 
 
 def _kv_cache_dims(k_cache, v_cache, n_kv, head_dim, quant_group, head_major):
     """(batch, L) of a pair of 4-bit caches."""
     row = wide_kv_quant_row_bytes(head_dim, quant_group)
-    torch = _torch()
-    for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
-        if c.dtype != torch.uint8 or c.dim() != 4 or c.shape[3] != row or c.shape[1 if head_major else 2] != n_kv:
-            raise ValueError(f"{name} must be uint8 [batch][{'n_kv][L' if head_major else 'L][n_kv'}][{row}]")
-    if k_cache.shape != v_cache.shape:
-        raise ValueError("k_cache and v_cache differ in shape")
-    return k_cache.shape[0], k_cache.shape[2 if head_major else 1]
+    shape, u8 = k_cache.shape, _torch().uint8
+    if len(shape) != 4 or shape[3] != row or shape[1 if head_major else 2] != n_kv or k_cache.dtype != u8:
+        raise ValueError(f"k_cache must be uint8 [batch][{'n_kv][L' if head_major else 'L][n_kv'}][{row}]")
+    if v_cache.shape != shape or v_cache.dtype != u8:
+        raise ValueError("v_cache must be like k_cache")
+    return shape[0], shape[2 if head_major else 1]
 
 
 def _per_seq(name, t, n):
@@ -452,17 +469,17 @@ def wide_kv_quantize(k, v, k_cache, v_cache, n_kv, head_dim, quant_group, pos=No
     each, None: 0 and L.  Returns (k_cache, v_cache)."""
     dev = _gpu(k, v, k_cache, v_cache, pos, kv_len)
     n_seq, L = _kv_cache_dims(k_cache, v_cache, n_kv, head_dim, quant_group, head_major)
-    if v.dtype != k.dtype or v.shape != k.shape or k.dim() != 2 or k.shape[1] != n_kv * head_dim:
+    shape = k.shape
+    if v.dtype != k.dtype or v.shape != shape or len(shape) != 2 or shape[1] != n_kv * head_dim:
         raise ValueError("k and v must be [n_seq*T][n_kv*head_dim] of one dtype")
-    if k.shape[0] % n_seq if n_seq else k.shape[0]:
+    T = shape[0] // n_seq if n_seq else 0
+    if T * n_seq != shape[0]:
         raise ValueError("k and v rows must split evenly into the caches' sequences")
     _per_seq("pos", pos, n_seq)
     _per_seq("kv_len", kv_len, n_seq)
-    with _on(dev):
-        _check("wide_kv_quantize", lib().wide_kv_quantize(
-            _dtype_code(k), n_seq, k.shape[0] // n_seq if n_seq else 0, L, n_kv, head_dim, quant_group,
-            KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, _p(pos), _p(kv_len), _p(k), _p(v), _p(k_cache),
-            _p(v_cache), _stream(k)))
+    _launch("wide_kv_quantize", dev, _dtype_code(k), n_seq, T, L, n_kv, head_dim, quant_group,
+            KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, _ptr(pos), _ptr(kv_len), k.data_ptr(), v.data_ptr(),
+            k_cache.data_ptr(), v_cache.data_ptr())
     return k_cache, v_cache
 
 
@@ -477,21 +494,19 @@ def wide_kv_dequantize(k_cache, v_cache, T, n_kv, head_dim, quant_group, pos=Non
     if T < 0:
         raise ValueError("T must be >= 0")
     if dtype is None:
-        dtype = torch.bfloat16 if k is None and v is None else (k if k is not None else v).dtype
+        dtype = k.dtype if k is not None else v.dtype if v is not None else torch.bfloat16
     shape = (n_seq * T, n_kv * head_dim)
     if k is None:
-        k = torch.empty(shape, dtype=dtype, device=dev)
+        k = torch.empty(shape, dtype=dtype, device=k_cache.device)
     if v is None:
-        v = torch.empty(shape, dtype=dtype, device=dev)
-    if any(t.dtype != dtype or t.shape != shape for t in (k, v)):
+        v = torch.empty(shape, dtype=dtype, device=k_cache.device)
+    if k.dtype != dtype or v.dtype != dtype or k.shape != shape or v.shape != shape:
         raise ValueError(f"k and v must be {dtype} [{shape[0]}][{shape[1]}]")
     _per_seq("pos", pos, n_seq)
     _per_seq("kv_len", kv_len, n_seq)
-    with _on(dev):
-        _check("wide_kv_dequantize", lib().wide_kv_dequantize(
-            _dtype_code(k), n_seq, T, L, n_kv, head_dim, quant_group,
-            KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, _p(pos), _p(kv_len), _p(k_cache), _p(v_cache), _p(k),
-            _p(v), _stream(k)))
+    _launch("wide_kv_dequantize", dev, _dtype_code(k), n_seq, T, L, n_kv, head_dim, quant_group,
+            KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, _ptr(pos), _ptr(kv_len), k_cache.data_ptr(),
+            v_cache.data_ptr(), k.data_ptr(), v.data_ptr())
     return k, v
 
 
@@ -505,6 +520,7 @@ def wide_attention_decode_kvq(q, k_cache, v_cache, mask, n_q, n_kv, head_dim, gr
     wide_kv_quantize leaves them).  q [B][n_q*head_dim] bf16; mask
     [B][n_groups] uint8; kv_len optional int32 [B].  Returns o, same shape as
     q."""
+    torch = _torch()
     dev = _gpu(q, k_cache, v_cache, mask, kv_len, o, ws)
     mask = _mask_bytes(mask)
     B, L = _kv_cache_dims(k_cache, v_cache, n_kv, head_dim, quant_group, head_major)
@@ -514,17 +530,15 @@ def wide_attention_decode_kvq(q, k_cache, v_cache, mask, n_q, n_kv, head_dim, gr
         raise ValueError("mask must be [batch][n_q*head_dim/group_size]")
     _per_seq("kv_len", kv_len, B)
     if o is None:
-        o = _torch().empty_like(q)
+        o = torch.empty_like(q)
     elif o.dtype != q.dtype or o.shape != q.shape:
         raise ValueError("o must be like q")
-    with _on(dev):
-        if ws is None:
-            need = wide_attention_decode_kvq_workspace_size(B, L, n_q, n_kv, head_dim, group_size, quant_group)
-            # (shapes the library rejects: no workspace, the call reports why)
-            ws = None if need == SIZE_MAX else _workspace(need, dev)
-        nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-        _check("wide_attention_decode_kvq", lib().wide_attention_decode_kvq(
-            _dtype_code(q), B, L, n_q, n_kv, head_dim, group_size, quant_group, _p(mask), _p(kv_len),
-            KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, _p(q), _p(k_cache), _p(v_cache), _p(o), _p(ws), nbytes,
-            _stream(q)))
+    if ws is None:
+        need = wide_attention_decode_kvq_workspace_size(B, L, n_q, n_kv, head_dim, group_size, quant_group)
+        # (shapes the library rejects: no workspace, the call reports why)
+        ws = None if need == SIZE_MAX else _workspace(need, q.device)
+    _launch("wide_attention_decode_kvq", dev, _dtype_code(q), B, L, n_q, n_kv, head_dim, group_size, quant_group,
+            mask.data_ptr(), _ptr(kv_len), KV_HEAD_MAJOR if head_major else KV_TOKEN_MAJOR, q.data_ptr(),
+            k_cache.data_ptr(), v_cache.data_ptr(), o.data_ptr(), _ptr(ws),
+            0 if ws is None else ws.numel() * ws.element_size())
     return o

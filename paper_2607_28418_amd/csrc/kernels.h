@@ -295,6 +295,9 @@ int attn_decode_waves(int64_t B, int n_kv, int L);  // 0: no balanced split for 
 hipError_t launch_attention_decode(AttnDecArgs a, hipStream_t s);
 
 // ---- 4-bit KV cache (kv_quant.hip, attention_decode_kvq.hip)
+struct FastDiv {
+  uint32_t mul, shift;
+};
 struct KvqArgs {
   const void* k;            // [n_seq*T][n_kv*128] bf16 or fp32 (written by the dequantiser)
   const void* v;
@@ -305,8 +308,10 @@ struct KvqArgs {
   int64_t n_seq;
   int T, L, n_kv, ng;       // ng = 128 / quant_group: 1, 2 or 4
   int head_major;
+  FastDiv by_heads, by_T;   // set by the launch, as is
+  uint32_t blocks;          // row blocks
 };
-hipError_t launch_kv_quant(const KvqArgs& a, bool f32, bool read, hipStream_t s);
+hipError_t launch_kv_quant(KvqArgs a, bool f32, bool read, hipStream_t s);
 // Decode attention; a.k and a.v are the 4-bit caches, quant_groups per row 1, 2
 // or 4.  a.table and a.part (of the waves that share the work) as for the bf16
 // cache's balanced split; no table: one workgroup per pair.

@@ -18,8 +18,13 @@
 // NaN, an infinity or a magnitude of 2^127 or more reads back as NaN (below that
 // no low, scale or value read back overflows).
 //
-// Both kernels are bound by memory: sixteen lanes per row, eight consecutive
-// dimensions (one 16-byte load or store in bf16) each.
+// Sixteen lanes per row, eight consecutive dimensions (one 16-byte load or store
+// in bf16) each; many small workgroups hide the loads (two or four rows a lane,
+// loaded together, ran 8-15% slower).  Reading back is bound by memory (8 x 32768
+// positions of 8 heads in bf16, 1.36 GB: 270 us, 5.0 TB/s, the rate of a copy);
+// quantising, by the vector ALUs as much: exact decisions cost five fp32
+// operations an element where every x - low is exact (nearly always, in bf16;
+// all of it in fp64 took 22 us instead of 15 for 8192 positions), fp64 elsewhere.
 #include <algorithm>
 
 #include "common.h"
@@ -29,34 +34,46 @@
 namespace wide {
 namespace {
 
-constexpr int kQT = 256;           // threads per workgroup: 16 rows
-constexpr int kQRows = kQT / 16;
+constexpr int kQT = 256;           // threads per workgroup
+constexpr int kQRows = kQT / 16;   // rows of a row block
 
-// Where row r of a call lies.  Token-major: rows in (token, KV head) order,
-// the order of both sides.  Head-major: (KV head, token) order, so that a
-// workgroup's rows are neighbours in the cache.
+// n / d for n < 2^31 (d from 1 to 2^31 - 1): Granlund and Montgomery's
+// multiplication by a rounded-up reciprocal.
+__device__ __forceinline__ uint32_t div_by(uint32_t n, FastDiv f) { return (__umulhi(f.mul, n) + n) >> f.shift; }
+
+// Where this lane's row of row block `blk` lies (sixteen rows).  Token-major:
+// rows in (token, KV head) order, the order of both sides.  Head-major: sixteen
+// tokens of one head, neighbours in the cache, the heads in turn so that
+// workgroups side by side touch whole rows of the K/V tensors (one head after
+// the other wrote one eighth of every 4 KB: 19 us instead of 15 for 8192 fp32
+// rows of 8 heads).
 struct Place {
   int64_t in;      // row of the K/V tensors, (token, head) order
   int64_t cache;   // row of the cache
-  bool live;       // 0 <= position < min(kv_len, L)
+  bool some;       // there is such a row
+  bool live;       // and 0 <= position < min(kv_len, L)
 };
 template <bool HM>
-__device__ __forceinline__ Place place(const KvqArgs& a, uint32_t r) {
-  const uint32_t tokens = (uint32_t)a.n_seq * (uint32_t)a.T;
+__device__ __forceinline__ Place place(const KvqArgs& a, uint32_t blk) {
+  const uint32_t tokens = (uint32_t)(a.n_seq * a.T), sub = threadIdx.x / 16;
   uint32_t t, h;
+  Place pl;
   if (HM) {
-    h = r / tokens;
-    t = r - h * tokens;
+    const uint32_t tile = div_by(blk, a.by_heads);
+    h = blk - tile * (uint32_t)a.n_kv;
+    t = tile * kQRows + sub;
   } else {
-    t = r / (uint32_t)a.n_kv;
+    const uint32_t r = min(blk * kQRows + sub, tokens * (uint32_t)a.n_kv);  // (past the last block: no row)
+    t = div_by(r, a.by_heads);
     h = r - t * (uint32_t)a.n_kv;
   }
-  const uint32_t b = t / (uint32_t)a.T;
+  pl.some = t < tokens;
+  t = min(t, tokens - 1);
+  const uint32_t b = div_by(t, a.by_T);
   const int64_t p = (int64_t)(t - b * (uint32_t)a.T) + (a.pos ? a.pos[b] : 0);
   const int len = a.kv_len ? min(a.kv_len[b], a.L) : a.L;
-  Place pl;
   pl.in = (int64_t)t * a.n_kv + h;
-  pl.live = p >= 0 && p < len;
+  pl.live = pl.some && p >= 0 && p < len;
   pl.cache = HM ? ((int64_t)b * a.n_kv + h) * a.L + p : ((int64_t)b * a.L + p) * a.n_kv + h;
   return pl;
 }
@@ -68,6 +85,10 @@ template <int D>
 __device__ __forceinline__ float row_xchg(float x) {
   constexpr int ctrl = D == 1 ? 0xB1 : D == 2 ? 0x4E : D == 4 ? 0x141 : 0x140;
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), ctrl, 0xF, 0xF, true));
+}
+template <int D>
+__device__ __forceinline__ uint32_t row_xchg_u(uint32_t x) {
+  return __float_as_uint(row_xchg<D>(__uint_as_float(x)));
 }
 template <int N>  // row_ror:N
 __device__ __forceinline__ uint32_t row_ror(uint32_t x) {
@@ -86,84 +107,151 @@ __device__ __forceinline__ float group_scale(double w) {
   return s < 0x1p-126 ? 0.0f : (float)s;
 }
 
+// What a lane finds of its eight values x: their group's scale and low (bf16 bits)
+// and the codes, two a word (16 bits each).  NaN groups: scale 0, low NaN.
+struct Coded {
+  uint32_t scale, low, code[4];
+};
+
+// Every step in fp64 where a rounding could change a decision.
+template <bool CUT>
+__device__ __forceinline__ Coded code_fp64(const float (&x)[8], float lo, float hi, bool bad) {
+  uint32_t lbits = __float_as_uint(lo);
+  if (CUT) {  // towards -inf: a negative number's size grows for the bits cut off
+    const uint32_t cut = lbits & 0xffff0000u;
+    lbits = (lbits >> 31) && cut != lbits ? cut + 0x10000u : cut;
+  }
+  const double low = (double)__uint_as_float(lbits);
+  const float s = bad ? 0.0f : group_scale((double)hi - low);
+  const float inv = s > 0.0f ? 1.0f / s : 0.0f, lf = __uint_as_float(lbits);
+  const double sd = (double)s, half = 0.5 * sd;
+  uint32_t code[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    // the nearest code up to fp32 rounding, then the exact remainder decides
+    float kf = rintf((x[e] - lf) * inv);
+    kf = s > 0.0f ? fminf(fmaxf(kf, 0.0f), 15.0f) : 0.0f;
+    const double rem = fma(-sd, (double)kf, (double)x[e] - low);
+    int c = (int)kf;
+    if (s > 0.0f && (fabs(rem) > half || (fabs(rem) == half && (c & 1)))) c += rem > 0.0 ? 1 : -1;
+    code[e] = (uint32_t)min(max(c, 0), 15);
+  }
+  Coded o;
+  o.scale = __float_as_uint(s) >> 16;
+  o.low = bad ? 0x7fc0u : lbits >> 16;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o.code[e] = code[2 * e] | code[2 * e + 1] << 16;
+  return o;
+}
+
+// The same decisions in fp32 for bf16 values whose differences x - low, and
+// hi - low, are exact.  With w and t = x - low exact in 24 bits and s in 8, the
+// correctly rounded quotients w / 15 and t / s never fall on a border (between
+// two bf16 values, between two codes) that the exact ones do not: a numerator
+// that misses the border's multiple misses it by an ulp of its own, and an ulp
+// over s < 2^(e+1), or over 15 < 2^4, is more than half an ulp of the quotient.
+// q + r / s with r the exact remainder is that quotient (Markstein).
+__device__ __forceinline__ Coded code_fp32(const float (&x)[8], float lo, float hi) {
+  const float w = hi - lo, c15 = 1.0f / 15.0f, q15 = w * c15;
+  uint32_t sb = __float_as_uint(fmaf(fmaf(-15.0f, q15, w), c15, q15));
+  sb = (sb + 0x7fffu + ((sb >> 16) & 1u)) & 0xffff0000u;
+  const float s = __uint_as_float(sb), inv = s > 0.0f ? 1.0f / s : 0.0f;
+  uint32_t k[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float t = x[e] - lo, q = t * inv;
+    k[e] = __float_as_uint(fmaf(fmaf(-s, q, t), inv, q) + 0x1.8p23f);  // the code in the low bits, ties to even
+  }
+  Coded o;
+  o.scale = sb >> 16;
+  o.low = __float_as_uint(lo) >> 16;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o.code[e] = __builtin_amdgcn_perm(k[2 * e + 1], k[2 * e], 0x05040100u);
+  return o;
+}
+
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 min2(u16x2 a, u16x2 b) { return __builtin_elementwise_min(a, b); }
+__device__ __forceinline__ u16x2 max2(u16x2 a, u16x2 b) { return __builtin_elementwise_max(a, b); }
+
 template <class T, int NG, bool HM>
 __global__ __launch_bounds__(kQT) void wide_kv_quantize(KvqArgs a) {
   constexpr int LPG = 16 / NG;  // lanes per group
+  constexpr bool F32 = sizeof(T) == 4;
   const int i = threadIdx.x & 15, m = i >> 2, qd = i & 3;
   const T* src = static_cast<const T*>(blockIdx.y ? a.v : a.k);
   uint8_t* cache = static_cast<uint8_t*>(blockIdx.y ? a.v_cache : a.k_cache);
-  const uint32_t rows = (uint32_t)a.n_seq * (uint32_t)a.T * (uint32_t)a.n_kv;
-  for (uint64_t r = (uint64_t)blockIdx.x * kQRows + threadIdx.x / 16; r < rows; r += (uint64_t)gridDim.x * kQRows) {
-    const Place pl = place<HM>(a, (uint32_t)r);
+  for (uint32_t blk = blockIdx.x; blk < a.blocks; blk += gridDim.x) {
+    const Place pl = place<HM>(a, blk);
     if (!pl.live) continue;  // (the same for all sixteen lanes of a row)
-    float x[8];
     const T* p = src + pl.in * 128 + 8 * i;
-    if constexpr (sizeof(T) == 2) {
-      const u32x4 w = ldg16(p);
+    u32x4 w[F32 ? 2 : 1];
+    w[0] = ldg16(p);
+    if constexpr (F32) w[1] = ldg16(p + 4);
+    float x[8];
+    bool bad, wide;  // a value at 2^127 or beyond, or not a number; differences that may not be exact
+    if constexpr (F32) {
+      float odd = 0.0f;  // NaN where a value's double is not finite
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[2 * e] = __uint_as_float(w[e] << 16);
-        x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+      for (int e = 0; e < 8; ++e) {
+        x[e] = __uint_as_float(w[e / 4][e % 4]);
+        odd = fmaf(x[e] + x[e], 0.0f, odd);
       }
+      odd += row_xchg<1>(odd);
+      odd += row_xchg<2>(odd);
+      odd += row_xchg<4>(odd);
+      odd += row_xchg<8>(odd);
+      bad = odd != 0.0f;
+      wide = true;
     } else {
-      const u32x4 w0 = ldg16(p), w1 = ldg16(p + 4);
+      u16x2 big = {0, 0}, small = {0xffff, 0xffff};  // of the sizes; zeros wrap to the top for the least
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        x[e] = __uint_as_float(w0[e]);
-        x[4 + e] = __uint_as_float(w1[e]);
+        x[2 * e] = __uint_as_float(w[0][e] << 16);
+        x[2 * e + 1] = __uint_as_float(w[0][e] & 0xffff0000u);
+        const u16x2 size = __builtin_bit_cast(u16x2, w[0][e] & 0x7fff7fffu);
+        big = max2(big, size);
+        small = min2(small, size - (u16x2){1, 1});
       }
+      uint32_t top = max(big[0], big[1]), least = min(small[0], small[1]);
+      top = max(top, row_xchg_u<1>(top)); least = min(least, row_xchg_u<1>(least));
+      top = max(top, row_xchg_u<2>(top)); least = min(least, row_xchg_u<2>(least));
+      top = max(top, row_xchg_u<4>(top)); least = min(least, row_xchg_u<4>(least));
+      top = max(top, row_xchg_u<8>(top)); least = min(least, row_xchg_u<8>(least));
+      bad = top >= 0x7f00u;
+      // exact while no size is below 2^-15 of the row's largest, which is not
+      // near the smallest numbers (2^-60: the remainders are exact, too)
+      wide = bad || top < (67u << 7) || least + 1 < top - (15u << 7);
     }
-    float lo = x[0], hi = x[0], odd = 0.0f;  // odd: NaN where a value's double is not finite
+    float lo = x[0], hi = x[0];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 1; e < 8; ++e) {
       lo = fminf(lo, x[e]);
       hi = fmaxf(hi, x[e]);
-      odd = fmaf(x[e] + x[e], 0.0f, odd);
     }
-    lo = fminf(lo, row_xchg<1>(lo)); hi = fmaxf(hi, row_xchg<1>(hi)); odd += row_xchg<1>(odd);
-    lo = fminf(lo, row_xchg<2>(lo)); hi = fmaxf(hi, row_xchg<2>(hi)); odd += row_xchg<2>(odd);
-    odd += row_xchg<4>(odd);
-    odd += row_xchg<8>(odd);
+    lo = fminf(lo, row_xchg<1>(lo)); hi = fmaxf(hi, row_xchg<1>(hi));
+    lo = fminf(lo, row_xchg<2>(lo)); hi = fmaxf(hi, row_xchg<2>(hi));
     if (LPG >= 8) { lo = fminf(lo, row_xchg<4>(lo)); hi = fmaxf(hi, row_xchg<4>(hi)); }
     if (LPG >= 16) { lo = fminf(lo, row_xchg<8>(lo)); hi = fmaxf(hi, row_xchg<8>(hi)); }
-    uint32_t lbits = __float_as_uint(lo);
-    if (sizeof(T) == 4) {  // towards -inf: a negative number's size grows for the bits cut off
-      const uint32_t cut = lbits & 0xffff0000u;
-      lbits = (lbits >> 31) && cut != lbits ? cut + 0x10000u : cut;
-    }
-    const double low = (double)__uint_as_float(lbits);
-    float s = group_scale((double)hi - low);
-    if (odd != 0.0f) {  // (NaN)
-      s = 0.0f;
-      lbits = 0x7fc00000u;
-    }
-    const float inv = s > 0.0f ? 1.0f / s : 0.0f, lf = __uint_as_float(lbits);
-    const double sd = (double)s, half = 0.5 * sd;
-    uint32_t code[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      // the nearest code up to fp32 rounding, then the exact remainder decides
-      float kf = rintf((x[e] - lf) * inv);
-      kf = s > 0.0f ? fminf(fmaxf(kf, 0.0f), 15.0f) : 0.0f;
-      const double rem = fma(-sd, (double)kf, (double)x[e] - low);
-      int c = (int)kf;
-      if (s > 0.0f && (fabs(rem) > half || (fabs(rem) == half && (c & 1)))) c += rem > 0.0 ? 1 : -1;
-      code[e] = (uint32_t)min(max(c, 0), 15);
-    }
-    uint32_t w[4];
+    Coded c;
+    if (wide) c = code_fp64<F32>(x, lo, hi, bad);
+    else c = code_fp32(x, lo, hi);
+    // word 4 qd + e of the row: nibbles m and m + 4 from this lane, the other
+    // groups' from the lanes four, eight and twelve away
+    uint32_t v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      w[e] = (code[2 * e] | code[2 * e + 1] << 16) << (4 * m);
-      w[e] |= row_ror<4>(w[e]);
-      w[e] |= row_ror<8>(w[e]);
+      v[e] = c.code[e] << (4 * m);
+      v[e] |= row_ror<4>(v[e]);
+      v[e] |= row_ror<8>(v[e]);
     }
     uint8_t* row = cache + pl.cache * (64 + 4 * NG);
-    const uint32_t mine = m == 0 ? w[0] : m == 1 ? w[1] : m == 2 ? w[2] : w[3];
+    const uint32_t mine = m == 0 ? v[0] : m == 1 ? v[1] : m == 2 ? v[2] : v[3];
     *reinterpret_cast<uint32_t*>(row + 16 * qd + 4 * m) = mine;
     if (i % LPG == 0) {
       uint16_t* meta = reinterpret_cast<uint16_t*>(row + 64);
-      meta[i / LPG] = (uint16_t)(__float_as_uint(s) >> 16);
-      meta[NG + i / LPG] = (uint16_t)(lbits >> 16);
+      meta[i / LPG] = (uint16_t)c.scale;
+      meta[NG + i / LPG] = (uint16_t)c.low;
     }
   }
 }
@@ -176,21 +264,25 @@ __global__ __launch_bounds__(kQT) void wide_kv_dequantize(KvqArgs a) {
   const int i = threadIdx.x & 15, m = i >> 2, qd = i & 3;
   T* dst = static_cast<T*>(const_cast<void*>(blockIdx.y ? a.v : a.k));
   const uint8_t* cache = static_cast<const uint8_t*>(blockIdx.y ? a.v_cache : a.k_cache);
-  const uint32_t rows = (uint32_t)a.n_seq * (uint32_t)a.T * (uint32_t)a.n_kv;
-  for (uint64_t r = (uint64_t)blockIdx.x * kQRows + threadIdx.x / 16; r < rows; r += (uint64_t)gridDim.x * kQRows) {
-    const Place pl = place<HM>(a, (uint32_t)r);
-    float y[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  for (uint32_t blk = blockIdx.x; blk < a.blocks; blk += gridDim.x) {
+    const Place pl = place<HM>(a, blk);
+    if (!pl.some) continue;
+    u32x4 w = {0, 0, 0, 0};
+    uint16_t sb = 0, lb = 0;
     if (pl.live) {
       const uint8_t* row = cache + pl.cache * (64 + 4 * NG);
-      const u32x4 w = *reinterpret_cast<const u32x4_a4*>(row + 16 * qd);
+      w = *reinterpret_cast<const u32x4_a4*>(row + 16 * qd);
       const uint16_t* meta = reinterpret_cast<const uint16_t*>(row + 64);
-      const float s = bf16_to_f32(meta[i / LPG]), low = bf16_to_f32(meta[NG + i / LPG]);
+      sb = meta[i / LPG];
+      lb = meta[NG + i / LPG];
+    }
+    const float s = bf16_to_f32(sb), low = bf16_to_f32(lb);
+    float y[8];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t c = w[e] >> (4 * m);
-        y[2 * e] = fmaf(s, (float)(c & 15u), low);
-        y[2 * e + 1] = fmaf(s, (float)(c >> 16 & 15u), low);
-      }
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t c = w[e] >> (4 * m);
+      y[2 * e] = fmaf(s, (float)(c & 15u), low);
+      y[2 * e + 1] = fmaf(s, (float)(c >> 16 & 15u), low);
     }
     T* p = dst + pl.in * 128 + 8 * i;
     if constexpr (sizeof(T) == 2) {
@@ -205,10 +297,19 @@ __global__ __launch_bounds__(kQT) void wide_kv_dequantize(KvqArgs a) {
 
 }  // namespace
 
-hipError_t launch_kv_quant(const KvqArgs& a, bool f32, bool read, hipStream_t s) {
-  const int64_t rows = a.n_seq * a.T * a.n_kv;
-  if (rows == 0) return hipSuccess;
-  const dim3 grid((unsigned)std::min<int64_t>((rows + kQRows - 1) / kQRows, 1 << 20), 2);
+static FastDiv fast_div(uint32_t d) {
+  uint32_t l = 0;
+  while (l < 32 && (uint64_t(1) << l) < d) ++l;
+  return FastDiv{(uint32_t)(((uint64_t(1) << 32) * ((uint64_t(1) << l) - d)) / d + 1), l};
+}
+
+hipError_t launch_kv_quant(KvqArgs a, bool f32, bool read, hipStream_t s) {
+  const int64_t tokens = a.n_seq * a.T;
+  if (tokens == 0) return hipSuccess;
+  a.by_heads = fast_div((uint32_t)a.n_kv);
+  a.by_T = fast_div((uint32_t)a.T);
+  a.blocks = (uint32_t)(a.head_major ? (tokens + kQRows - 1) / kQRows * a.n_kv : (tokens * a.n_kv + kQRows - 1) / kQRows);
+  const dim3 grid(std::min(a.blocks, 1u << 22), 2);
 #define WIDE_KVQ(T, NG, HM)                                                                               \
   do {                                                                                                    \
     if (read) WIDE_LAUNCH_NAMED("wide_kv_dequantize", (wide_kv_dequantize<T, NG, HM>), grid, dim3(kQT), 0, s, a); \

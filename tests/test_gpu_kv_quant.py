@@ -128,6 +128,25 @@ def test_quantize_special_rows(dtype, qg):
         assert torch.equal(y.nan_to_num(7.0), ref.nan_to_num(7.0))
 
 
+@pytest.mark.parametrize("qg", [32, 64, 128])
+@pytest.mark.parametrize("spread", [3, 14, 17, 40])
+def test_quantize_borders(qg, spread):
+    """Values of three bits with exponents far apart: many lie on the border of
+    two codes, or miss it by what an fp32 difference does not hold."""
+    g = np.random.default_rng(spread)
+    rows = 2000
+    x = g.integers(-7, 8, (rows, HD)) * 2.0 ** -g.integers(0, spread + 1, (rows, HD))
+    x[:, ::7] = g.integers(-15, 16, (rows, x[:, ::7].shape[1])) * 0.25
+    for dtype in (torch.bfloat16, torch.float32):
+        t = torch.from_numpy(x.astype(np.float32)).to(dtype)
+        assert (t.double().numpy() == x).all()
+        kc = torch.zeros(1, rows, 1, _kvq.row_bytes(qg), dtype=torch.uint8, device="cuda")
+        vc = kc.clone()
+        W.wide_kv_quantize(t.cuda(), -t.cuda(), kc, vc, 1, HD, qg)
+        assert np.array_equal(kc.cpu().numpy()[0, :, 0], _kvq.quantize(x, qg))
+        assert np.array_equal(vc.cpu().numpy()[0, :, 0], _kvq.quantize(-x, qg))
+
+
 # ---- reading back ------------------------------------------------------------------
 
 @pytest.mark.parametrize("hm", [False, True])
