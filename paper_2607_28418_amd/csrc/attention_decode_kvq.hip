@@ -7,15 +7,16 @@
 // Nothing is dequantised.
 //
 // A wave takes tiles of 32 keys of one (sequence, KV head) pair, straight into
-// registers, and the KV head's query heads in sets of four.  Short contexts:
-// one workgroup per pair, its waves take tiles in turn, meet in LDS and store
+// registers, and all query heads of the KV head.  Short contexts: one workgroup per pair, its waves take tiles in turn, meet in LDS and store
 // o.  Longer ones: every wave takes an equal run of the active pairs' tiles
 // (decode_split.h) and leaves a (maximum, sum, unnormalised o) per pair it
 // meets; a second kernel joins them.
 //
-// The MFMAs' sixteen columns (rows, for P.V) are (head h of the set, 32-wide
-// group g of the dimensions), 4 h + g, so that a scale multiplies a value of
-// one group where it stands and no lane repeats another's work.  Per tile:
+// The MFMAs' sixteen columns (rows, for P.V) are (head h, 32-wide group g of the
+// dimensions): 4 heads x 4 groups, 8 x 2 in two sets (groups 0 and 1, 2 and 3) or
+// 16 x 1 in four, by the query heads per KV head, so that a scale multiplies a
+// value of one group where it stands and no lane repeats another's work.  Per
+// tile and set:
 //   scores  D[key][h, g] = c . q over group g, one 16x16x128 fp8 MFMA per 16
 //           keys: a byte 0000cccc is the e4m3 number c 2^-9, so a mask (and a
 //           shift) makes operands of the codes; q as two e4m3 terms (its eight
@@ -23,15 +24,15 @@
 //           scale takes back) with zeros outside group g.  The scales s_g[key]
 //           come in the same layout from a 16x16x16 bf16 MFMA of the rows'
 //           (scale, low) with a one-hot operand, low_g sum(q)_g from one with
-//           sum(q) in three bf16 parts (24 bits).  The four groups' sums meet
-//           within the lanes of a quad, which share out the four keys of each;
+//           sum(q) in three bf16 parts (24 bits).  The sets are added, then the
+//           groups within the lanes of a head, which share out their four keys;
 //   softmax online per head, fp32.  The maximum moves only when a score passes
 //           it by 8 (in the exponent), so p <= 2^8, and most tiles rescale
 //           nothing;
 //   P.V     p s_g [h, g][key] in two bf16 parts (2^-16 relative), two MFMAs for
-//           each nibble of the words; 16 + c is a bf16 with exponent 2^4 and the
-//           code in its top mantissa bits: a shift and an and-or make two.  Row
-//           (h, g) holds dimensions of group g in nibbles g and g + 4 only.
+//           each nibble of the words, with the set of its group; 16 + c is a bf16
+//           with exponent 2^4 and the code in its top mantissa bits: a shift and
+//           an and-or make two.  Row (h, g) of nibble n counts where g = n mod 4.
 // The low terms of P.V are fp32 sums per (head, group) beside it.
 #include <algorithm>
 
@@ -86,14 +87,38 @@ __device__ __forceinline__ f32x4 mfma_codes(i32x8 a, i32x8 b, f32x4 c, int b_sca
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 127 + 9, 0, b_scale);
 }
 
-// Lane l ^ D of each quad; lane R of each quad.
+// Lane l ^ D of each quad; lane R of each quad, of each pair of lanes.
 template <int D>
 __device__ __forceinline__ float quad_xor(float x) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), D == 1 ? 0xB1 : 0x4E, 0xF, 0xF, true));
 }
 template <int R>
+__device__ __forceinline__ float pair_bcast(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), R == 0 ? 0xA0 : 0xF5, 0xF, 0xF, true));
+}
+template <int R>
 __device__ __forceinline__ float quad_bcast(float x) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), R * 0x55, 0xF, 0xF, true));
+}
+
+// f(r, p of row r) for the four rows of a lane whose head's GC lanes hold the
+// rows r = v GC + (lane of the head).
+template <int GC, class F>
+__device__ __forceinline__ void head_rows(const float (&p)[4 / GC], F f) {
+  if constexpr (GC == 4) {
+    f(0, quad_bcast<0>(p[0]));
+    f(1, quad_bcast<1>(p[0]));
+    f(2, quad_bcast<2>(p[0]));
+    f(3, quad_bcast<3>(p[0]));
+  } else if constexpr (GC == 2) {
+    f(0, pair_bcast<0>(p[0]));
+    f(1, pair_bcast<1>(p[0]));
+    f(2, pair_bcast<0>(p[1]));
+    f(3, pair_bcast<1>(p[1]));
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) f(r, p[r]);
+  }
 }
 
 template <int NG>
@@ -104,20 +129,23 @@ struct Tile {
   u32x2 vm[2];        // as km
 };
 
-// NS sets of four query heads (the KV head has at most 4 NS).  Tiles at keys j,
-// j + step, .. below j1 (at least one), for the heads act() of pair (b, hkv).
+// H (4, 8 or 16) at least the query heads per KV head.  Tiles at keys j, j + step,
+// .. below j1 (at least one), for the heads act() of pair (b, hkv).
 // emit(head, maximum, sum) and store(head, dim, o[dim], o[dim + 1]) receive the
 // unnormalised result.
-template <int NG, int NS, class Act, class Emit, class Store>
+template <int NG, int H, class Act, class Emit, class Store>
 __device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, Act act_of, int j, int step, int j1,
                                        Emit emit, Store store) {
   constexpr int R = 64 + 4 * NG;       // bytes of a cache row
+  constexpr int GC = 16 / H;           // groups of a set
+  constexpr int NS = H / 4;            // sets
+  constexpr int V = 4 / GC;            // of a 16-key half's scores, those one lane goes on with
   const int lane = lane_id(), l16 = lane & 15, g4 = lane >> 4;
-  const int g = l16 & 3, hl = l16 >> 2;  // this lane's column: group, head of the set
+  const int h = l16 / GC, gl = l16 % GC;  // this lane's column: head, group of the set
   u32x4 qr[NS];
 #pragma unroll
   for (int s = 0; s < NS; ++s)
-    qr[s] = ldg16(a.q + ((int64_t)b * a.n_q + hkv * a.qpk + min(4 * s + hl, a.qpk - 1)) * 128 + 32 * g + 8 * g4);
+    qr[s] = ldg16(a.q + ((int64_t)b * a.n_q + hkv * a.qpk + min(h, a.qpk - 1)) * 128 + 32 * (s * GC + gl) + 8 * g4);
   // ---- loads: a view per tile of the rows up to j1; rows past them read zeros
   const uint32_t ld = a.head_major ? R : (uint32_t)a.n_kv * R;
   const int64_t base = a.head_major ? ((int64_t)b * a.n_kv + hkv) * a.L * R
@@ -151,13 +179,12 @@ __device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, Act
   // ---- operands that stay
   const uint32_t act = act_of();
   i32x8 q_hi[NS], q_lo[NS];            // q 2^e in two e4m3 terms, the second times 2^5
-  int q_sc[NS];                        // the exponent byte that undoes e
   u32x2 b_low[NS][2];                  // sum(q) of (h, g) in three parts, at the place of low_g
+  u32x2 b_s[NS], b_lo[NS];             // one-hot: the place of s_g, and of low_g with -16 at s_g
   auto pk = [](float x, float y) { return __float_as_uint(x) >> 16 | (__float_as_uint(y) & 0xffff0000u); };
-  // the one-hot operands: the place of s_g, and of low_g with -16 at s_g
-  constexpr int GQ = 4 / NG;
-  const int slot = g / GQ;             // the quantisation group of this column
-  auto place = [&](float s, float low) {  // (scale place of this column's group) = s, (low place) = low
+  // (scale place of group 32 g's quantisation group) = s, (low place) = low
+  auto place = [&](int g, float s, float low) {
+    const int slot = g / (4 / NG);
     if constexpr (NG == 4) {
       const float x = g4 & 1 ? low : s;
       return u32x2{pk(slot == 0 ? x : 0.0f, slot == 1 ? x : 0.0f), pk(slot == 2 ? x : 0.0f, slot == 3 ? x : 0.0f)};
@@ -167,80 +194,79 @@ __device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, Act
       return u32x2{pk(s, low), 0u};
     }
   };
-  const float first = g4 < (NG == 4 ? 2 : 1) ? 1.0f : 0.0f;  // (each place counts once)
-  const u32x2 b_s = place(first, 0.0f), b_lo = place(-16.0f * first, first);
+  const bool on = h < a.qpk && ((act >> h) & 1u);
+  float mx = 0.0f;
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
-    const bool on = 4 * s + hl < a.qpk && ((act >> (4 * s + hl)) & 1u);
-    float x[8], mx = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t w = on ? qr[s][e] : 0u;
-      x[2 * e] = __uint_as_float(w << 16);
-      x[2 * e + 1] = __uint_as_float(w & 0xffff0000u);
+      qr[s][e] = on ? qr[s][e] : 0u;
+      mx = fmaxf(mx, fmaxf(fabsf(__uint_as_float(qr[s][e] << 16)), fabsf(__uint_as_float(qr[s][e] & 0xffff0000u))));
     }
+  }
+  if (GC >= 2) mx = fmaxf(mx, quad_xor<1>(mx));
+  if (GC >= 4) mx = fmaxf(mx, quad_xor<2>(mx));
+  mx = fmaxf(mx, __shfl_xor(mx, 16));
+  mx = fmaxf(mx, __shfl_xor(mx, 32));
+  // max |q| 2^e in [128, 256); tiny heads: as far up as the scale byte goes
+  const int e2 = min(134 - (int)(__float_as_uint(mx) >> 23), 122);
+  const int q_sc = 127 - e2;           // the exponent byte that undoes e
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      mx = fmaxf(mx, fabsf(x[e]));
-      sum += x[e];
+  for (int s = 0; s < NS; ++s) {
+    const int g = s * GC + gl;
+    float x[8], sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(qr[s][e] << 16);
+      x[2 * e + 1] = __uint_as_float(qr[s][e] & 0xffff0000u);
+      sum += x[2 * e] + x[2 * e + 1];
     }
-    mx = fmaxf(mx, quad_xor<1>(mx));
-    mx = fmaxf(mx, quad_xor<2>(mx));
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    // max |q| 2^e in [128, 256); tiny heads: as far up as the scale byte goes
-    const int e2 = min(134 - (int)(__float_as_uint(mx) >> 23), 122);
-    q_sc[s] = 127 - e2;
-    i32x8 hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float y0 = __builtin_amdgcn_ldexpf(x[2 * i], e2), y1 = __builtin_amdgcn_ldexpf(x[2 * i + 1], e2);
-      const int h = __builtin_amdgcn_cvt_pk_fp8_f32(y0, y1, 0, false);
-      const int l = __builtin_amdgcn_cvt_pk_fp8_f32(32.0f * (y0 - __builtin_amdgcn_cvt_f32_fp8(h, 0)),
-                                                    32.0f * (y1 - __builtin_amdgcn_cvt_f32_fp8(h, 1)), 0, false);
+      const int hi = __builtin_amdgcn_cvt_pk_fp8_f32(y0, y1, 0, false);
+      const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(32.0f * (y0 - __builtin_amdgcn_cvt_f32_fp8(hi, 0)),
+                                                     32.0f * (y1 - __builtin_amdgcn_cvt_f32_fp8(hi, 1)), 0, false);
       // nibble g of word 4 (l/16) + i: byte g / 2 of the even or the odd nibbles; nibble g + 4 two bytes on
       const int sh = g & 2 ? 8 : 0;
-      const int hb = ((h & 0xff) | (h & 0xff00) << 8) << sh, lb = ((l & 0xff) | (l & 0xff00) << 8) << sh;
-      hi[i] = g & 1 ? 0 : hb;
-      hi[4 + i] = g & 1 ? hb : 0;
-      lo[i] = g & 1 ? 0 : lb;
-      lo[4 + i] = g & 1 ? lb : 0;
+      const int hb = ((hi & 0xff) | (hi & 0xff00) << 8) << sh, lb = ((lo & 0xff) | (lo & 0xff00) << 8) << sh;
+      q_hi[s][i] = g & 1 ? 0 : hb;
+      q_hi[s][4 + i] = g & 1 ? hb : 0;
+      q_lo[s][i] = g & 1 ? 0 : lb;
+      q_lo[s][4 + i] = g & 1 ? lb : 0;
     }
-    q_hi[s] = hi;
-    q_lo[s] = lo;
     // sum = p0 + p1 + p2, eight bits each
     const float p0 = __uint_as_float(__float_as_uint(sum) & 0xffff0000u), r1 = sum - p0;
     const float p1 = __uint_as_float(__float_as_uint(r1) & 0xffff0000u), p2 = r1 - p1;
     if constexpr (NG == 4) {
-      b_low[s][0] = place(0.0f, g4 == 1 ? p0 : p1);
-      b_low[s][1] = place(0.0f, g4 == 1 ? p2 : 0.0f);
+      b_low[s][0] = place(g, 0.0f, g4 == 1 ? p0 : p1);
+      b_low[s][1] = place(g, 0.0f, g4 == 1 ? p2 : 0.0f);
     } else {
-      b_low[s][0] = place(0.0f, g4 == 0 ? p0 : g4 == 1 ? p1 : g4 == 2 ? p2 : 0.0f);
+      b_low[s][0] = place(g, 0.0f, g4 == 0 ? p0 : g4 == 1 ? p1 : g4 == 2 ? p2 : 0.0f);
     }
+    const float first = g4 < (NG == 4 ? 2 : 1) ? 1.0f : 0.0f;  // (each place counts once)
+    b_s[s] = place(g, first, 0.0f);
+    b_lo[s] = place(g, -16.0f * first, first);
   }
 
   const float sc = a.scale_log2, slack = 8.0f / sc;
-  // of head (set, hl): the maximum, m sc, this lane's share of the sum
-  float m[NS], msc[NS], z[NS];
+  float m = -INFINITY, msc = -INFINITY, z = 0.0f;  // of head h: the maximum, m sc, this lane's share of the sum
   float lo[NS];                        // of column (h, g): this lane's share of sum p (low - 16 s)
-  f32x4 acc[NS][8];                    // [row 4 (l/16) + group][word l16] of nibble n
+  f32x4 acc[8];                        // nibble n: [row 4 (l/16) + r][word l16]
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    m[s] = msc[s] = -INFINITY;
-    z[s] = lo[s] = 0.0f;
+  for (int s = 0; s < NS; ++s) lo[s] = 0.0f;
 #pragma unroll
-    for (int n = 0; n < 8; ++n) acc[s][n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+  for (int n = 0; n < 8; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const f32x4 zero = {0.0f, 0.0f, 0.0f, 0.0f};
   uint32_t sixteens = 0x41804180u;
   asm("" : "+v"(sixteens));
-  const bool odd = g & 1, upper = g & 2;
+  const bool odd = gl & 1, upper = gl & 2;
 
   auto process = [&](int j, const Tile<NG>& T) {
     i32x8 A[2];
-    f32x4 ks[2], vs[2], vl[2];
+    f32x4 x[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -248,67 +274,90 @@ __device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, Act
         A[t][i] = (int)(T.kc[t][i] & 0x0f0f0f0fu);
         A[t][4 + i] = (int)((T.kc[t][i] >> 4) & 0x0f0f0f0fu);
       }
-      ks[t] = mfma16k16(T.km[t], b_s, zero);
-      vs[t] = mfma16k16(T.vm[t], b_s, zero);
-      vl[t] = mfma16k16(T.vm[t], b_lo, zero);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        f32x4 D = mfma_codes(A[t], q_hi[s], zero, q_sc);
+        D = mfma_codes(A[t], q_lo[s], D, q_sc - 5);
+        const f32x4 ks = mfma16k16(T.km[t], b_s[s], zero);
+        f32x4 y = mfma16k16(T.km[t], b_low[s][0], zero);
+        if (NG == 4) y = mfma16k16(T.km[t], b_low[s][1], y);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = fmaf(D[r], ks[r], y[r]);
+        x[t] = s == 0 ? y : x[t] + y;
+      }
+    }
+    // S[t][v]: row r = v GC + gl of half t, key 16t + 4 (l/16) + r
+    float S[2][V], top = -INFINITY;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if constexpr (GC == 1) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[t][r] = x[t][r];
+      } else {
+        const float y0 = (odd ? x[t][1] : x[t][0]) + quad_xor<1>(odd ? x[t][0] : x[t][1]);
+        const float y1 = (odd ? x[t][3] : x[t][2]) + quad_xor<1>(odd ? x[t][2] : x[t][3]);
+        if constexpr (GC == 2) {
+          S[t][0] = y0;
+          S[t][1] = y1;
+        } else {
+          S[t][0] = (upper ? y1 : y0) + quad_xor<2>(upper ? y0 : y1);
+        }
+      }
+    }
+    if (j + kTile > j1) {  // the last tile
+      asm volatile("");    // (a branch, not instructions in every tile)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (j + 16 * t + 4 * g4 + v * GC + gl >= j1) S[t][v] = -INFINITY;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int v = 0; v < V; ++v) top = fmaxf(top, S[t][v]);
+    if (__any(top > m + slack)) {
+      if (GC >= 2) top = fmaxf(top, quad_xor<1>(top));
+      if (GC >= 4) top = fmaxf(top, quad_xor<2>(top));
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m, top), ms = mn * sc;
+      const float al = mn == m ? 1.0f : __builtin_amdgcn_exp2f(msc - ms);
+      m = mn;
+      msc = ms;
+      z *= al;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) lo[s] *= al;
+#pragma unroll
+      for (int r = 0; r < 4; r += GC) {  // (a head's rows)
+        const float ar = __shfl(al, 4 * g4 + r);
+#pragma unroll
+        for (int n = 0; n < 8; ++n) acc[n][r + (n & 3) % GC] *= ar;
+      }
     }
     u32x4 P1[NS], P2[NS];              // p s, first and second part
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      float S[2];                      // of key 16t + 4 (l/16) + g
+    for (int t = 0; t < 2; ++t) {
+      float p[V];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        f32x4 D = mfma_codes(A[t], q_hi[s], zero, q_sc[s]);
-        D = mfma_codes(A[t], q_lo[s], D, q_sc[s] - 5);
-        f32x4 x = mfma16k16(T.km[t], b_low[s][0], zero);
-        if (NG == 4) x = mfma16k16(T.km[t], b_low[s][1], x);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) x[r] = fmaf(D[r], ks[t][r], x[r]);
-        const float y0 = (odd ? x[1] : x[0]) + quad_xor<1>(odd ? x[0] : x[1]);
-        const float y1 = (odd ? x[3] : x[2]) + quad_xor<1>(odd ? x[2] : x[3]);
-        S[t] = (upper ? y1 : y0) + quad_xor<2>(upper ? y0 : y1);
-      }
-      if (j + kTile > j1) {  // the last tile
-        asm volatile("");    // (a branch, not instructions in every tile)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-          if (j + 16 * t + 4 * g4 + g >= j1) S[t] = -INFINITY;
-      }
-      float mx = fmaxf(S[0], S[1]);
-      if (__any(mx > m[s] + slack)) {
-        mx = fmaxf(mx, quad_xor<1>(mx));
-        mx = fmaxf(mx, quad_xor<2>(mx));
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float mn = fmaxf(m[s], mx), ms = mn * sc;
-        const float al = mn == m[s] ? 1.0f : __builtin_amdgcn_exp2f(msc[s] - ms);
-        m[s] = mn;
-        msc[s] = ms;
-        z[s] *= al;
-        lo[s] *= al;
-        const float ar = __shfl(al, 4 * g4);  // of the head this lane's rows belong to
-#pragma unroll
-        for (int n = 0; n < 8; ++n) acc[s][n][n & 3] *= ar;
+      for (int v = 0; v < V; ++v) {
+        p[v] = __builtin_amdgcn_exp2f(fmaf(S[t][v], sc, -msc));
+        z += p[v];
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(S[t], sc, -msc[s]));
-        z[s] += p;
-        float x[4], y[4];
-        x[0] = quad_bcast<0>(p) * vs[t][0];
-        x[1] = quad_bcast<1>(p) * vs[t][1];
-        x[2] = quad_bcast<2>(p) * vs[t][2];
-        x[3] = quad_bcast<3>(p) * vs[t][3];
-        lo[s] = fmaf(quad_bcast<0>(p), vl[t][0], lo[s]);
-        lo[s] = fmaf(quad_bcast<1>(p), vl[t][1], lo[s]);
-        lo[s] = fmaf(quad_bcast<2>(p), vl[t][2], lo[s]);
-        lo[s] = fmaf(quad_bcast<3>(p), vl[t][3], lo[s]);
+      for (int s = 0; s < NS; ++s) {
+        const f32x4 vs = mfma16k16(T.vm[t], b_s[s], zero), vl = mfma16k16(T.vm[t], b_lo[s], zero);
+        float ps[4], rest[4];
+        head_rows<GC>(p, [&](int r, float pr) {
+          ps[r] = pr * vs[r];
+          lo[s] = fmaf(pr, vl[r], lo[s]);
+        });
 #pragma unroll
-        for (int r = 0; r < 4; ++r) y[r] = x[r] - __uint_as_float(__float_as_uint(x[r]) & 0xffff0000u);
+        for (int r = 0; r < 4; ++r) rest[r] = ps[r] - __uint_as_float(__float_as_uint(ps[r]) & 0xffff0000u);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          P1[s][2 * t + h] = __builtin_amdgcn_perm(__float_as_uint(x[2 * h + 1]), __float_as_uint(x[2 * h]), 0x07060302u);
-          P2[s][2 * t + h] = pack_bf16x2_hw(y[2 * h], y[2 * h + 1]);
+        for (int i = 0; i < 2; ++i) {
+          P1[s][2 * t + i] = __builtin_amdgcn_perm(__float_as_uint(ps[2 * i + 1]), __float_as_uint(ps[2 * i]), 0x07060302u);
+          P2[s][2 * t + i] = pack_bf16x2_hw(rest[2 * i], rest[2 * i + 1]);
         }
       }
     }
@@ -317,9 +366,9 @@ __device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, Act
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        wl[2 * t + h] = __builtin_amdgcn_perm(T.vc[t][2 * h + 1], T.vc[t][2 * h], 0x05040100u);
-        wh[2 * t + h] = __builtin_amdgcn_perm(T.vc[t][2 * h + 1], T.vc[t][2 * h], 0x07060302u);
+      for (int i = 0; i < 2; ++i) {
+        wl[2 * t + i] = __builtin_amdgcn_perm(T.vc[t][2 * i + 1], T.vc[t][2 * i], 0x05040100u);
+        wh[2 * t + i] = __builtin_amdgcn_perm(T.vc[t][2 * i + 1], T.vc[t][2 * i], 0x07060302u);
       }
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
@@ -332,11 +381,8 @@ __device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, Act
                : (n & 3) == 2 ? codes<2>(w, sixteens)
                               : codes<3>(w, sixteens);
       }
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        acc[s][n] = mfma16(P1[s], B, acc[s][n]);
-        acc[s][n] = mfma16(P2[s], B, acc[s][n]);
-      }
+      acc[n] = mfma16(P1[(n & 3) / GC], B, acc[n]);
+      acc[n] = mfma16(P2[(n & 3) / GC], B, acc[n]);
     }
   };
 
@@ -349,20 +395,21 @@ __device__ __forceinline__ void attend(const AttnDecArgs& a, int b, int hkv, Act
   }
   if (j < j1) process(j, t0);
 
+  if (GC >= 2) z += quad_xor<1>(z);
+  if (GC >= 4) z += quad_xor<2>(z);
+  z += __shfl_xor(z, 16);
+  z += __shfl_xor(z, 32);
+  if (g4 == 0 && gl == 0 && h < a.qpk) emit(h, msc, z);
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
-    float zs = z[s], ls = lo[s];
-    zs += quad_xor<1>(zs);
-    zs += quad_xor<2>(zs);
-    zs += __shfl_xor(zs, 16);
-    zs += __shfl_xor(zs, 32);
+    float ls = lo[s];
     ls += __shfl_xor(ls, 16);
     ls += __shfl_xor(ls, 32);
-    if (g4 == 0 && g == 0 && 4 * s + hl < a.qpk) emit(4 * s + hl, msc[s], zs);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const float l = __shfl(ls, 4 * g4 + n);
-      store(4 * s + g4, 32 * n + 2 * l16, acc[s][n][n] + l, acc[s][4 + n][n] + l);
+    for (int r = 0; r < 4; ++r) {      // row (h, g) of set s
+      const float l = __shfl(ls, 4 * g4 + r);
+      const int g = s * GC + r % GC;
+      store((4 * g4 + r) / GC, 32 * g + 2 * l16, acc[g][r] + l, acc[4 + g][r] + l);
     }
   }
 }
@@ -375,9 +422,9 @@ __device__ __forceinline__ uint32_t active_mask(const AttnDecArgs& a, int b, int
 }
 
 // One workgroup of NW waves per pair.
-template <int NG, int NS, int NW>
-__global__ __launch_bounds__(NW * 64, NS < 4 ? 2 : 1) void wide_attn_decode_kvq(AttnDecArgs a) {
-  __shared__ float s_o[NW][4 * NS][128 + 4];
+template <int NG, int H, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void wide_attn_decode_kvq(AttnDecArgs a) {
+  __shared__ float s_o[NW][H][128 + 4];
   __shared__ float s_m[NW][16], s_z[NW][16];
   const int w = wave_id(), p = xcd_remap(blockIdx.x, gridDim.x), b = p / a.n_kv, hkv = p - b * a.n_kv;
   const int len = seq_len(a, b);
@@ -388,7 +435,7 @@ __global__ __launch_bounds__(NW * 64, NS < 4 ? 2 : 1) void wide_attn_decode_kvq(
     return;
   }
   if (w * kTile < len)
-    attend<NG, NS>(
+    attend<NG, H>(
         a, b, hkv, [&] { return act; }, w * kTile, NW * kTile, len,
         [&](int h, float m, float z) {
           s_m[w][h] = m;
@@ -416,8 +463,8 @@ __global__ __launch_bounds__(NW * 64, NS < 4 ? 2 : 1) void wide_attn_decode_kvq(
 constexpr int kPart = 4 + 128;  // floats of a partial: maximum, sum, (two unused), o
 
 // Equal runs of tiles a wave.
-template <int NG, int NS>
-__global__ __launch_bounds__(kSplitThreads, NS < 4 ? 2 : 1) void wide_attn_decode_kvq_runs(AttnDecArgs a) {
+template <int NG, int H>
+__global__ __launch_bounds__(kSplitThreads, 2) void wide_attn_decode_kvq_runs(AttnDecArgs a) {
   extern __shared__ uint64_t s_pre[];  // tiles and active pairs before each pair
   __shared__ uint64_t s_sum[kSplitThreads / kWave + 1];
   list_units<kTile, kKvqMinTiles>(a, s_pre, s_sum);
@@ -436,7 +483,7 @@ __global__ __launch_bounds__(kSplitThreads, NS < 4 ? 2 : 1) void wide_attn_decod
     const int b = p / a.n_kv, hkv = p - b * a.n_kv;
     const int j1 = __builtin_amdgcn_readfirstlane((int)min((int64_t)seq_len(a, b), (int64_t)(u_end - pre(p)) * kTile));
     float* part = a.part + (int64_t)(wave + rank) * a.qpk * kPart;
-    attend<NG, NS>(
+    attend<NG, H>(
         a, b, hkv, [&] { return active_mask(a, b, hkv); }, j, kTile, j1,
         [&](int h, float m, float z) {
           part[h * kPart] = m;
@@ -463,8 +510,8 @@ struct SeqSplit {
   uint32_t act;   // active KV heads
   int first;      // waves before the sequence
 };
-template <int NG, int NS>
-__global__ __launch_bounds__(kSplitThreads, NS < 4 ? 2 : 1) void wide_attn_decode_kvq_seqs(AttnDecArgs a) {
+template <int NG, int H>
+__global__ __launch_bounds__(kSplitThreads, 2) void wide_attn_decode_kvq_seqs(AttnDecArgs a) {
   extern __shared__ SeqSplit s_seq[];  // B + 1
   __shared__ int s_cnt[kSplitThreads / kWave][kWave];
   __shared__ int64_t s_red[kSplitThreads / kWave][2];
@@ -576,7 +623,7 @@ __global__ __launch_bounds__(kSplitThreads, NS < 4 ? 2 : 1) void wide_attn_decod
   const int j = (int)((int64_t)nt * c / r) * kTile;
   const int j1 = min(seq_len(a, b), (int)min((int64_t)nt * (c + 1) / r * kTile, (int64_t)a.L));
   float* part = a.part + (int64_t)wave * a.qpk * kPart;
-  attend<NG, NS>(
+  attend<NG, H>(
       a, b, hkv, [&] { return active_mask(a, b, hkv); }, j, kTile, __builtin_amdgcn_readfirstlane(j1),
       [&](int h, float m, float z) {
         part[h * kPart] = m;
@@ -690,28 +737,28 @@ hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStrea
   // half as many as the waves.
   a.by_seq = !a.head_major && a.n_kv > 1 && a.n_kv <= 32 && a.B * a.n_kv <= a.waves / 2;
   const int pairs = a.B * a.n_kv, lds = (pairs + 1) * (int)sizeof(uint64_t);
-#define WIDE_DEC4(NG, NS)                                                                                    \
+#define WIDE_DEC4(NG, H)                                                                                     \
   do {                                                                                                       \
-    constexpr int NW = NS < 4 ? 8 : 4;                                                                       \
+    constexpr int NW = 8;                                                                                    \
     if (a.table && a.by_seq)                                                                                 \
-      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_seqs<NG, NS>), dim3(a.waves / 4),      \
+      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_seqs<NG, H>), dim3(a.waves / 4),      \
                         dim3(kSplitThreads), (a.B + 1) * (int)sizeof(SeqSplit), s, a);                       \
     else if (a.table)                                                                                        \
-      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_runs<NG, NS>), dim3(a.waves / 4),      \
+      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_runs<NG, H>), dim3(a.waves / 4),      \
                         dim3(kSplitThreads), lds, s, a);                                                     \
     else                                                                                                     \
-      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq<NG, NS, NW>), dim3(pairs), dim3(NW * 64), \
+      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq<NG, H, NW>), dim3(pairs), dim3(NW * 64), \
                         0, s, a);                                                                            \
   } while (0)
-#define WIDE_DEC4_NG(NS)                        \
+#define WIDE_DEC4_NG(H)                         \
   do {                                          \
-    if (quant_groups == 4) WIDE_DEC4(4, NS);    \
-    else if (quant_groups == 2) WIDE_DEC4(2, NS); \
-    else WIDE_DEC4(1, NS);                      \
+    if (quant_groups == 4) WIDE_DEC4(4, H);    \
+    else if (quant_groups == 2) WIDE_DEC4(2, H); \
+    else WIDE_DEC4(1, H);                      \
   } while (0)
-  if (a.qpk <= 4) WIDE_DEC4_NG(1);
-  else if (a.qpk <= 8) WIDE_DEC4_NG(2);
-  else WIDE_DEC4_NG(4);
+  if (a.qpk <= 4) WIDE_DEC4_NG(4);
+  else if (a.qpk <= 8) WIDE_DEC4_NG(8);
+  else WIDE_DEC4_NG(16);
 #undef WIDE_DEC4_NG
 #undef WIDE_DEC4
   const hipError_t e = hipGetLastError();
