@@ -506,122 +506,128 @@ __global__ __launch_bounds__(kSplitThreads, 2) void wide_attn_decode_kvq_runs(At
 // into r = ceil(tiles / q) equal chunks, waves in (sequence, chunk, head) order,
 // neighbouring workgroups on one XCD; q is the least number of tiles for which
 // all of it fits the resident waves.  One partial a wave, in slot `wave`.
+constexpr int kSeqMaxPairs = kAttnDecWaves / 2;  // (pairs that share the waves)
 struct SeqSplit {
-  uint32_t act;   // active KV heads
-  int first;      // waves before the sequence
+  uint32_t act;  // active KV heads
+  int n;         // tiles
 };
+
+// ceil(n / q) where it is far below 2^22
+__device__ __forceinline__ int chunks_of(int n, int q, float inv) {
+  int r = (int)((float)n * inv);
+  r += n > r * q;
+  r -= (r - 1) * q >= n;
+  return r;
+}
+
 template <int NG, int H>
 __global__ __launch_bounds__(kSplitThreads, 2) void wide_attn_decode_kvq_seqs(AttnDecArgs a) {
-  extern __shared__ SeqSplit s_seq[];  // B + 1
-  __shared__ int s_cnt[kSplitThreads / kWave][kWave];
-  __shared__ int64_t s_red[kSplitThreads / kWave][2];
+  constexpr int W = kSplitThreads / kWave;
+  extern __shared__ SeqSplit s_seq[];  // B
+  __shared__ int s_cnt[W][kWave];
   const int tid = threadIdx.x, w = wave_id(), lane = lane_id(), P = a.B * a.n_kv;
-  auto tiles = [&](int b) { return (max(seq_len(a, b), 0) + kTile - 1) / kTile; };
-  for (int b = tid; b <= a.B; b += kSplitThreads) s_seq[b].act = 0;
-  __syncthreads();
-  for (int p = tid; p < P; p += kSplitThreads) {
-    const int b = p / a.n_kv, hkv = p - b * a.n_kv, h0 = hkv * a.qpk;
+  uint32_t on = 0;  // bit k: pair tid + k kSplitThreads is active
+#pragma unroll
+  for (int k = 0; k < kSeqMaxPairs / kSplitThreads; ++k) {
+    const int p = tid + k * kSplitThreads;
+    if (p >= P) break;
+    const int b = p / a.n_kv, h0 = (p - b * a.n_kv) * a.qpk;
     const uint8_t* mrow = a.mask + (int64_t)b * a.ng;
     const int g0 = h0 / a.hpg, g1 = (h0 + a.qpk - 1) / a.hpg;
-    uint32_t on = mrow[g0];
-    for (int g = g0 + 1; g <= g1; ++g) on |= mrow[g];
-    if (on) atomicOr(&s_seq[b].act, 1u << hkv);
+    uint32_t any = mrow[g0];
+    for (int g = g0 + 1; g <= g1; ++g) any |= mrow[g];
+    if (any) on |= 1u << k;
   }
+  for (int b = tid; b < a.B; b += kSplitThreads)
+    s_seq[b] = SeqSplit{0u, (max(seq_len(a, b), 0) + kTile - 1) / kTile};
   __syncthreads();
-  // all tiles, and the heads that have any
-  const int per = (a.B + kSplitThreads - 1) / kSplitThreads, b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
-  int64_t all = 0, heads = 0;
-  for (int b = b0; b < b1; ++b) {
-    const int n = tiles(b), A = __popc(s_seq[b].act);
-    all += (int64_t)n * A;
+#pragma unroll
+  for (int k = 0; k < kSeqMaxPairs / kSplitThreads; ++k)
+    if ((on >> k) & 1u) {
+      const int p = tid + k * kSplitThreads, b = p / a.n_kv;
+      atomicOr(&s_seq[b].act, 1u << (p - b * a.n_kv));
+    }
+  __syncthreads();
+  // all tiles, and the heads that have any (every wave for itself)
+  int all = 0, heads = 0;
+  for (int b = lane; b < a.B; b += kWave) {
+    const int n = s_seq[b].n, A = __popc(s_seq[b].act);
+    all += n * A;
     heads += n > 0 ? A : 0;
   }
 #pragma unroll
   for (int d = 32; d >= 1; d >>= 1) {
-    all += __shfl_xor((long long)all, d);
-    heads += __shfl_xor((long long)heads, d);
-  }
-  if (lane == 0) {
-    s_red[w][0] = all;
-    s_red[w][1] = heads;
-  }
-  __syncthreads();
-  all = heads = 0;
-#pragma unroll
-  for (int i = 0; i < kSplitThreads / kWave; ++i) {
-    all += s_red[i][0];
-    heads += s_red[i][1];
+    all += __shfl_xor(all, d);
+    heads += __shfl_xor(heads, d);
   }
   // q: sum A ceil(n / q) <= all / q + heads, so hi fits if the heads do (they are
   // at most half of the waves: the caller's rule); 64 candidates from the mean up
-  const int lo_q = max((int)((all + a.waves - 1) / a.waves), kKvqMinTiles);
-  const int hi_q = max((int)((all + a.waves - heads - 1) / (a.waves - heads)), lo_q);
-  const int q_of = lo_q + (int)((int64_t)(hi_q - lo_q) * lane / (kWave - 1));
-  int cnt = 0;
-  for (int b = w; b < a.B; b += kSplitThreads / kWave) cnt += __popc(s_seq[b].act) * ((tiles(b) + q_of - 1) / q_of);
-  s_cnt[w][lane] = cnt;
-  __syncthreads();
-  cnt = 0;
+  const int lo_q = max((all + a.waves - 1) / a.waves, kKvqMinTiles);
+  const int hi_q = max((all + a.waves - heads - 1) / (a.waves - heads), lo_q);
+  int q = lo_q;
+  if (hi_q > lo_q) {
+    const int q_of = lo_q + (int)((int64_t)(hi_q - lo_q) * lane / (kWave - 1));
+    const float inv = 1.0f / (float)q_of;
+    int cnt = 0;
+    for (int b = w; b < a.B; b += W) cnt += __popc(s_seq[b].act) * chunks_of(s_seq[b].n, q_of, inv);
+    s_cnt[w][lane] = cnt;
+    __syncthreads();
+    cnt = 0;
 #pragma unroll
-  for (int i = 0; i < kSplitThreads / kWave; ++i) cnt += s_cnt[i][lane];
-  const uint64_t fits = __ballot(cnt <= a.waves);
-  const int q = __builtin_amdgcn_readlane(q_of, fits ? __builtin_ctzll(fits) : kWave - 1);
-  // waves before each sequence
-  int sum = 0;
-  for (int b = b0; b < b1; ++b) sum += __popc(s_seq[b].act) * ((tiles(b) + q - 1) / q);
-  int x = sum;
+    for (int i = 0; i < W; ++i) cnt += s_cnt[i][lane];
+    const uint64_t fits = __ballot(cnt <= a.waves);
+    q = __builtin_amdgcn_readlane(q_of, fits ? __builtin_ctzll(fits) : kWave - 1);
+  }
+  // the waves of each sequence, 64 sequences at a time; the waves that have work in
+  // all, and before each, come out of a second pass
+  const float inv = 1.0f / (float)q;
+  auto waves_of = [&](int b) { return b < a.B ? __popc(s_seq[b].act) * chunks_of(s_seq[b].n, q, inv) : 0; };
+  int total = 0;
+  for (int b = lane; b < a.B; b += kWave) total += waves_of(b);
 #pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  __syncthreads();
-  if (lane == kWave - 1) s_cnt[w][0] = x;
-  __syncthreads();
-  int run = x - sum, total = 0;
-#pragma unroll
-  for (int i = 0; i < kSplitThreads / kWave; ++i) {
-    if (i < w) run += s_cnt[i][0];
-    total += s_cnt[i][0];
-  }
-  for (int b = b0; b < b1; ++b) {
-    s_seq[b].first = run;
-    const uint32_t act = s_seq[b].act;
-    const int A = __popc(act), r = (tiles(b) + q - 1) / q;
-    if (blockIdx.x == 0)
-      for (int h = 0; h < a.n_kv; ++h) {
-        int32_t* t = a.table + 4 * ((int64_t)b * a.n_kv + h);
-        t[0] = run + __popc(act & ((1u << h) - 1));
-        t[1] = (act >> h) & 1u ? r : 0;
-        t[2] = A;
-      }
-    run += A * r;
-  }
-  if (tid == 0) s_seq[a.B].first = total;
-  __syncthreads();
-
+  for (int d = 32; d >= 1; d >>= 1) total += __shfl_xor(total, d);
   total = __builtin_amdgcn_readfirstlane(total);
-  const int nwg = (total + 3) / 4;
-  if ((int)blockIdx.x >= nwg) return;
-  const int wave = xcd_remap(blockIdx.x, nwg) * 4 + w;
-  if (wave >= total) return;
-  int b = 0, n = a.B;  // the last sequence with at most `wave` waves before it (it has some)
-  while (n > 1) {
-    const int st = (n + kWave - 1) / kWave, i = b + lane * st;
-    const uint64_t le = __ballot(lane * st < n && s_seq[min(i, a.B)].first <= wave);
-    const int k = 63 - __builtin_clzll(le);
-    n = min(st, n - k * st);
-    b += k * st;
-  }
-  b = __builtin_amdgcn_readfirstlane(b);
+  const int nwg = (total + W - 1) / W;
+  const bool lists = blockIdx.x == gridDim.x - 1 && w == 0;  // writes the merge's table
+  const int wave = (int)blockIdx.x < nwg ? xcd_remap(blockIdx.x, nwg) * W + w : total;
+  int mine = -1, at = 0, before = 0;
+  if (wave < total || lists)
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+      const int b = b0 + lane, cnt = waves_of(b);
+      int x = cnt;
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) {
+        const int y = __shfl_up(x, d);
+        if (lane >= d) x += y;
+      }
+      const int first = before + x - cnt;
+      const uint64_t here = __ballot(wave >= first && wave < first + cnt);
+      if (here) {
+        const int l = __builtin_ctzll(here);
+        mine = b0 + l;
+        at = wave - __builtin_amdgcn_readlane(first, l);
+      }
+      if (lists && b < a.B) {
+        const uint32_t act = s_seq[b].act;
+        const int A = __popc(act), r = A ? cnt / A : 0;
+        for (int h = 0; h < a.n_kv; ++h)
+          *reinterpret_cast<int4*>(a.table + 4 * ((int64_t)b * a.n_kv + h)) =
+              int4{first + __popc(act & ((1u << h) - 1)), (act >> h) & 1u ? r : 0, A, 0};
+      }
+      before += __builtin_amdgcn_readlane(x, kWave - 1);
+    }
+  if (mine < 0) return;
+  const int b = __builtin_amdgcn_readfirstlane(mine);
   uint32_t act = __builtin_amdgcn_readfirstlane(s_seq[b].act);
-  const int at = wave - __builtin_amdgcn_readfirstlane(s_seq[b].first), A = __popc(act);
-  const int c = at / A, k = at - c * A, nt = __builtin_amdgcn_readfirstlane(tiles(b)), r = (nt + q - 1) / q;
+  at = __builtin_amdgcn_readfirstlane(at);
+  const int A = __popc(act), nt = __builtin_amdgcn_readfirstlane(s_seq[b].n);
+  const int r = __builtin_amdgcn_readfirstlane(chunks_of(nt, q, inv));
+  const int c = at / A, k = at - c * A;
   for (int i = 0; i < k; ++i) act &= act - 1;
   const int hkv = __builtin_ctz(act);
-  // chunk c of r: tiles [nt c / r, nt (c + 1) / r)
-  const int j = (int)((int64_t)nt * c / r) * kTile;
-  const int j1 = min(seq_len(a, b), (int)min((int64_t)nt * (c + 1) / r * kTile, (int64_t)a.L));
+  // chunk c of r: nt / r tiles, one more in the first nt mod r
+  const int each = nt / r, more = nt - each * r, first = c * each + min(c, more);
+  const int j = first * kTile, j1 = min(seq_len(a, b), j + (each + (c < more)) * kTile);
   float* part = a.part + (int64_t)wave * a.qpk * kPart;
   attend<NG, H>(
       a, b, hkv, [&] { return active_mask(a, b, hkv); }, j, kTile, __builtin_amdgcn_readfirstlane(j1),
@@ -658,24 +664,26 @@ __global__ __launch_bounds__(SL == 2 ? 256 : SL * 32) void wide_attn_decode_kvq_
   const float* part = a.part + tab[0] * row + (h % a.qpk) * kPart;
   float m = -INFINITY, z = 0.0f;
   f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int c = sl; c < nseg; c += 4 * SL) {
-    float cm[4], cz[4];
-    f32x4 v[4];
+  constexpr int U = SL == 32 ? 8 : 4;  // segments whose loads go together
+  for (int c = sl; c < nseg; c += U * SL) {
+    float cm[U], cz[U], mn = m;
+    f32x4 v[U];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {  // four segments' loads together (past the end: the first one's, weight 0)
+    for (int u = 0; u < U; ++u) {  // (past the end: the first one's, weight 0)
       const bool in = c + SL * u < nseg;
       const float* q = part + (in ? c + SL * u : c) * ld;
       cm[u] = in ? q[0] : -INFINITY;
       cz[u] = q[1];
       v[u] = *reinterpret_cast<const f32x4*>(q + 4 + 4 * dq);
     }
-    const float mn = fmaxf(fmaxf(fmaxf(m, cm[0]), fmaxf(cm[1], cm[2])), cm[3]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) mn = fmaxf(mn, cm[u]);
     const float f0 = __builtin_amdgcn_exp2f(m - mn);
     z *= f0;
     o *= f0;
     m = mn;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < U; ++u) {
       if (c + SL * u >= nseg) break;  // (a weight of 0 times a NaN)
       const float f = __builtin_amdgcn_exp2f(cm[u] - mn);
       z = fmaf(f, cz[u], z);
@@ -733,16 +741,15 @@ size_t attn_decode_kvq_part_floats(int64_t B, int n_kv, int qpk, int waves) {
 
 hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStream_t s) {
   if (a.B == 0) return hipSuccess;
-  // Sequence by sequence: the KV heads fit one word, and all of them are at most
-  // half as many as the waves.
-  a.by_seq = !a.head_major && a.n_kv > 1 && a.n_kv <= 32 && a.B * a.n_kv <= a.waves / 2;
+  // Sequence by sequence: the KV heads fit one word.
+  a.by_seq = !a.head_major && a.n_kv > 1 && a.n_kv <= 32 && a.B * a.n_kv <= kSeqMaxPairs;
   const int pairs = a.B * a.n_kv, lds = (pairs + 1) * (int)sizeof(uint64_t);
 #define WIDE_DEC4(NG, H)                                                                                     \
   do {                                                                                                       \
     constexpr int NW = 8;                                                                                    \
     if (a.table && a.by_seq)                                                                                 \
       WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_seqs<NG, H>), dim3(a.waves / 4),      \
-                        dim3(kSplitThreads), (a.B + 1) * (int)sizeof(SeqSplit), s, a);                       \
+                        dim3(kSplitThreads), a.B * (int)sizeof(SeqSplit)      , s, a);                       \
     else if (a.table)                                                                                        \
       WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_runs<NG, H>), dim3(a.waves / 4),      \
                         dim3(kSplitThreads), lds, s, a);                                                     \
