@@ -1425,19 +1425,14 @@ wide_status_t attention_decode_kvq_shape(wide_dtype_t dt, int64_t B, int32_t L, 
   return WIDE_OK;
 }
 
-// Workspace of a call whose waves share the work: the pairs' segments, then the
-// segments' partials (the table alone, unused, otherwise).
+// Workspace of a call: the pairs' segments, then the segments' partials.
 struct KvqWS {
-  int waves = 0;
   int32_t* table = nullptr;
   float* part = nullptr;
 };
-size_t carve_attention_decode_kvq(Carve& c, int64_t B, int L, int nq, int nkv, KvqWS& w) {
-  if (B == 0) return 0;
-  w.waves = wide::attn_decode_kvq_waves(B, nkv, L);
-  w.table = c.take<int32_t>((size_t)B * nkv * 4);
-  if (w.waves) w.part = c.take<float>(wide::attn_decode_kvq_part_floats(B, nkv, nq / nkv, w.waves));
-  else w.table = nullptr;
+size_t carve_attention_decode_kvq(Carve& c, const wide::KvqPlan& p, KvqWS& w) {
+  w.table = c.take<int32_t>(std::max<size_t>(p.table_ints, 1));
+  w.part = c.take<float>(p.part_floats);
   return c.off;
 }
 
@@ -1471,9 +1466,16 @@ size_t wide_attention_decode_kvq_workspace_size(int64_t batch, int32_t L, int32_
   const bool bad = attention_decode_kvq_shape(WIDE_BF16, batch, L, n_q_heads, n_kv_heads, head_dim, group_size,
                                               quant_group, s) != WIDE_OK;
   g_last_error = keep;
-  Carve c(nullptr);
-  KvqWS w;
-  return bad ? SIZE_MAX : carve_attention_decode_kvq(c, batch, L, n_q_heads, n_kv_heads, w);
+  if (bad) return SIZE_MAX;
+  if (batch == 0) return 0;
+  size_t need = 0;
+  for (const int cut : {0, 1, 2}) {  // (whatever the layout and the groups)
+    Carve c(nullptr);
+    KvqWS w;
+    need = std::max(need, carve_attention_decode_kvq(c, wide::attn_decode_kvq_plan(batch, n_kv_heads, L,
+                                                         n_q_heads / n_kv_heads, cut == 0, cut == 1), w));
+  }
+  return need;
 }
 
 wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t L, int32_t n_q_heads,
@@ -1491,13 +1493,16 @@ wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t 
   CHECK(check_ptr(k_cache, "k_cache"));
   CHECK(check_ptr(v_cache, "v_cache"));
   CHECK(check_ptr(o, "o"));
+  const bool head_major = kv_layout == WIDE_KV_HEAD_MAJOR || n_kv_heads == 1;  // (the same rows)
+  const bool whole = (size_t)n_kv_heads * wide_kv_quant_row_bytes(head_dim, quant_group) % 16 == 0;
+  const wide::KvqPlan plan = wide::attn_decode_kvq_plan(batch, n_kv_heads, L, s.qpk, head_major, whole);
   KvqWS w;
   {
     Carve c0(nullptr);
-    CHECK(check_ws(ws, ws_bytes, carve_attention_decode_kvq(c0, batch, L, n_q_heads, n_kv_heads, w)));
+    CHECK(check_ws(ws, ws_bytes, carve_attention_decode_kvq(c0, plan, w)));
   }
   Carve c(ws);
-  carve_attention_decode_kvq(c, batch, L, n_q_heads, n_kv_heads, w);
+  carve_attention_decode_kvq(c, plan, w);
   wide::AttnDecArgs a{};
   a.q = static_cast<const uint16_t*>(q);
   a.k = static_cast<const uint16_t*>(k_cache);
@@ -1506,8 +1511,9 @@ wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t 
   a.mask = mask;
   a.kv_len = kv_len;
   a.part = w.part;
-  a.table = w.table;
-  a.waves = w.waves;
+  a.table = plan.waves || plan.wgs ? w.table : nullptr;
+  a.waves = plan.waves;
+  a.wgs = plan.wgs;
   a.B = (int)batch;
   a.L = L;
   a.n_q = n_q_heads;
@@ -1515,7 +1521,7 @@ wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t 
   a.ng = s.ng;
   a.hpg = s.hpg;
   a.qpk = s.qpk;
-  a.head_major = kv_layout == WIDE_KV_HEAD_MAJOR;
+  a.head_major = head_major;
   a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
   const hipError_t e = wide::launch_attention_decode_kvq(a, head_dim / quant_group, stream);
   if (e != hipSuccess) return hip_fail(e, "attention decode, 4-bit cache");

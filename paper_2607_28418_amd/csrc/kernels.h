@@ -285,7 +285,7 @@ struct AttnDecArgs {
   int waves;                // balanced split: waves sharing the work
   int B, L, n_q, n_kv, ng, hpg, qpk;
   int head_major;           // cache layout (see k)
-  int by_seq;               // (4-bit cache) the work is cut sequence by sequence: table [B * n_kv][4]
+  int wgs;                  // (4-bit cache) workgroups that read whole rows: table [B * n_kv][4]; 0: not so cut
   int chunk, n_chunks;      // keys per workgroup (multiple of 64), ceil(L / chunk)
   float scale_log2;
 };
@@ -313,12 +313,18 @@ struct KvqArgs {
 };
 hipError_t launch_kv_quant(KvqArgs a, bool f32, bool read, hipStream_t s);
 // Decode attention; a.k and a.v are the 4-bit caches, quant_groups per row 1, 2
-// or 4.  a.table and a.part (of the waves that share the work) as for the bf16
-// cache's balanced split; no table: one workgroup per pair.
-constexpr int kKvqMaxPairs = 2304;  // listed in LDS beside the tiles, two workgroups a CU
-constexpr int kKvqMinTiles = 2;     // 64 keys: the shortest run of a wave
-int attn_decode_kvq_waves(int64_t B, int n_kv, int L);
-size_t attn_decode_kvq_part_floats(int64_t B, int n_kv, int qpk, int waves);
+// or 4.  What its waves (workgroups) that share the work take of the workspace,
+// in a.table and a.part; neither: one workgroup per pair, no workspace.  whole:
+// a position's rows are a multiple of 16 bytes.
+constexpr int kKvqMaxPairs = 8000;   // listed in LDS, two workgroups a CU
+constexpr int kKvqMaxGroups = 512;   // of up to eight KV heads of a sequence, listed beside their rows
+constexpr int kKvqMinTiles = 2;      // 64 keys: the shortest run of a wave
+constexpr int kKvqWgs = 256;         // one a CU
+struct KvqPlan {
+  int waves, wgs;
+  size_t table_ints, part_floats;
+};
+KvqPlan attn_decode_kvq_plan(int64_t B, int n_kv, int L, int qpk, bool head_major, bool whole);
 hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStream_t s);
 
 hipError_t launch_gemv_n(const GVNArgs& a, bool swiglu, hipStream_t s);

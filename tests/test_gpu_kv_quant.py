@@ -299,6 +299,42 @@ def test_attention_batches(B, L, n_q, n_kv, group, qg, hm, ragged):
     assert torch.equal(o.view(torch.int16), run_attention(*args).view(torch.int16))  # the same call, the same bits
 
 
+@pytest.mark.parametrize("qg", [32, 64, 128])
+@pytest.mark.parametrize("B,L,n_q,n_kv,group,lens", [
+    (32, 2081, 32, 8, 512, "random"),          # whole rows of eight heads
+    (5, 7000, 64, 8, 1024, [6999, 0, 3501, 7000, 65]),
+    (9, 2100, 16, 16, 128, "random"),          # two sets of eight
+    (33, 2081, 12, 4, 384, "random"),
+    (64, 2081, 32, 2, 256, "random"),
+    (1, 33000, 8, 8, 128, None),
+    (300, 2049, 8, 8, 128, "random"),          # more groups than workgroups
+])
+def test_attention_token_major(B, L, n_q, n_kv, group, lens, qg):
+    """Long token-major caches, read by the position.  Before each call another has left NaN wherever a
+    workgroup keeps rows, so that what lies behind a sequence's end or belongs to a masked head shows."""
+    say("token-major", B, L, n_q, n_kv, group, qg)
+    g = np.random.default_rng(B + qg)
+    q = rows_f64(B, (B, n_q * HD), torch.bfloat16, spread=0.3)
+    mask = (g.random((B, n_q * HD // group)) < 0.6).astype(np.uint8)
+    mask[0, 0] = 1
+    kv_len = np.minimum(g.integers(0, L + 400, B) // 4 * (g.random(B) < 0.5) + 7, L).tolist() if lens == "random" else lens
+    if lens == "random":
+        kv_len[:2] = [L, 0]
+    few = 4                                                      # sequences with values of their own
+    kc, vc = make_cache(L, min(B, few), L, n_kv, qg, False)
+    kc, vc = (np.concatenate([c] * -(-B // few))[:B] for c in (kc, vc))
+    kd, vd = (d(poison(c, kv_len, mask, n_q, n_kv, group, False)) for c in (kc, vc))
+    nan = torch.full_like(kd, 0xff)
+    args = (q.cuda(), kd, vd, d(mask), n_q, n_kv, group, qg, i32(kv_len), False)
+    first = None
+    for _ in range(2):
+        run_attention(q.cuda(), nan, nan, d(np.ones_like(mask)), n_q, n_kv, group, qg, None, False)
+        o = run_attention(*args)
+        check_attention(o, q, kc, vc, mask, n_q, n_kv, group, qg, kv_len, False, (B, L, n_kv))
+        assert first is None or torch.equal(o.view(torch.int16), first.view(torch.int16))
+        first = o
+
+
 def test_cache_beyond_32_bit_offsets():
     """Rows more than 4 GiB into a cache: written, read back and attended to."""
     n_kv, qg, L = 32, 32, 1 << 20
