@@ -357,7 +357,7 @@ size_t wide_attention_decode_workspace_size(int64_t batch, int32_t L, int32_t n_
  *             pos = -padding; right padding: beyond kv_len) are skipped and no
  *             other byte of the caches changes.
  *   k, v      [n_seq*T][n_kv_heads*head_dim], as wide_qkvo_masked writes them.
- *   k_cache, v_cache  written; 16-byte aligned.
+ *   k_cache, v_cache  written; 16-byte aligned, two buffers.
  * Limit: n_seq*T*n_kv_heads < 2^31.  n_seq*T == 0 or L == 0 is a valid no-op.
  */
 wide_status_t wide_kv_quantize(wide_dtype_t dt, int64_t n_seq, int32_t T, int32_t L,
@@ -373,7 +373,7 @@ wide_status_t wide_kv_quantize(wide_dtype_t dt, int64_t n_seq, int32_t T, int32_
  * < min(kv_len[b], L), else +0.  (With pos[b] = kv_len[b] - T the sequences
  * end together and leftpad[b] = T - kv_len[b] is their padding.)
  * low + scale*code is formed in fp32 with one rounding; bf16 rows are rounded
- * once more.  n_seq*T == 0 is a valid no-op.
+ * once more.  k and v are two buffers.  n_seq*T == 0 is a valid no-op.
  */
 wide_status_t wide_kv_dequantize(wide_dtype_t dt, int64_t n_seq, int32_t T, int32_t L,
                                  int32_t n_kv_heads, int32_t head_dim, int32_t quant_group,
@@ -395,6 +395,11 @@ size_t wide_kv_quant_row_bytes(int32_t head_dim, int32_t quant_group);
  *   the rest     as for wide_attention_decode (len_b = min(kv_len[b], L), len_b
  *                <= 0 gives +0; cache rows at and past len_b are never used, nor
  *                is the cache of a (sequence, KV head) without an active head).
+ * Arithmetic: scores and sums in fp32, q to 2^-22 of the head's largest value and
+ * the probabilities times a row's scale to 2^-16 of themselves (two parts each);
+ * o is rounded to bf16.  Values of 2^100 and more can overflow the sums.  The same
+ * call gives the same bits; in large calls the order of a sequence's sums follows
+ * from the whole batch.
  * Limits (WIDE_ERR_UNSUPPORTED): batch*n_q_heads < 2^24, n_kv_heads <= 65536,
  * L <= 2^30.
  */

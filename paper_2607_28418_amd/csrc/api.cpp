@@ -1397,6 +1397,8 @@ wide_status_t kvq_rows(bool read, wide_dtype_t dt, int64_t n_seq, int32_t T, int
     CHECK(check_ptr(k_cache, "k_cache"));
     CHECK(check_ptr(v_cache, "v_cache"));
   }
+  if (read ? k == v : k_cache == v_cache)
+    return fail(WIDE_ERR_INVALID_ARG, "%s are the same", read ? "k and v" : "k_cache and v_cache");
   wide::KvqArgs a{};
   a.k = k;
   a.v = v;

@@ -21,8 +21,9 @@
 //   scores  D[key][h, g] = c . q over group g, one 16x16x128 fp8 MFMA per 16
 //           keys: a byte 0000cccc is the e4m3 number c 2^-9, so a mask (and a
 //           shift) makes operands of the codes; q as two e4m3 terms (its eight
-//           bits, both scaled by a power of two per head that the MFMA's block
-//           scale takes back) with zeros outside group g.  The scales s_g[key]
+//           bits, or what of them is above 2^-22 of the head's largest, scaled
+//           by a power of two per head that the MFMA's block scale takes back)
+//           with zeros outside group g.  The scales s_g[key]
 //           come in the same layout from a 16x16x16 bf16 MFMA of the rows'
 //           (scale, low) with a one-hot operand, low_g sum(q)_g from one with
 //           sum(q) in three bf16 parts (24 bits).  The sets are added, then the

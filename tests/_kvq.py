@@ -108,6 +108,10 @@ def attention(q, kc, vc, mask, n_q, n_kv, group, qg, kv_len, head_major):
         most 160 additions off by u of at most E = sum_d (47 s + |low|)|q|; one
         more rounding of the scaled exponent.  The three bf16 parts of sum(q)
         hold 24 bits of it: u of the same again.
+        Of q, its two e4m3 terms leave up to 2^-22 of the head's largest value
+        where a value is below 2^-14 of it: at most 15 s 2^-22 max|q| in each
+        dimension, no more than the sums' bound even if one dimension holds all
+        of |q| (15/47 * 128 * 4/162 = 1.0), and then the sums are short.
       p: exp2 to 2^-22 relative, times the error of its exponent; the maximum
         cancels in the quotient but for p's own exponent (twice the error).
       P.V: p s in two bf16 parts, 2^-16 of it, over terms up to (16 + 15) s p;

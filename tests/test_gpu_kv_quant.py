@@ -335,6 +335,51 @@ def test_attention_token_major(B, L, n_q, n_kv, group, lens, qg):
         first = o
 
 
+@pytest.mark.parametrize("B,hm", [(1000, True), (1001, True), (512, False), (513, False)])
+def test_attention_many_sequences(B, hm):
+    """The most (sequence, KV head) pairs that share their waves, and one sequence more."""
+    L, n_q, n_kv, group, qg = 2050, 8, 8, 128, 32
+    say("many sequences", B, hm)
+    g = np.random.default_rng(B)
+    q = rows_f64(B, (B, n_q * HD), torch.bfloat16, spread=0.3)
+    mask = (g.random((B, n_kv)) < 0.5).astype(np.uint8)
+    kv_len = np.where(g.random(B) < 0.1, L, g.integers(-1, 90, B))
+    which = g.integers(0, 4, B)                                  # the sequences' caches, of four
+    four = make_cache(5, 4, L, n_kv, qg, hm)
+    kd, vd = (d(c)[d(which)] for c in four)
+    o = run_attention(q.cuda(), kd, vd, d(mask), n_q, n_kv, group, qg, i32(kv_len), hm)
+    some = np.unique(np.r_[0, 1, B - 2, B - 1, np.flatnonzero(kv_len == L)[:4], g.integers(0, B, 20)])
+    kc, vc = (c[which[some]] for c in four)
+    check_attention(o[torch.from_numpy(some).cuda()], q[some], kc, vc, mask[some], n_q, n_kv, group, qg, kv_len[some], hm,
+                    (B, hm))
+    off = np.repeat(mask == 0, HD, axis=1) | (kv_len <= 0)[:, None]
+    assert not o.cpu()[torch.from_numpy(off)].any() and torch.isfinite(o).all()
+
+
+@pytest.mark.parametrize("L,hm", [(300, False), (3000, True), (33000, False)])
+@pytest.mark.parametrize("n_q", [8, 16, 32])
+def test_attention_not_finite_queries(n_q, L, hm):
+    """An infinity or a NaN in one query head gives that head NaN and no other anything; a masked head, zeros."""
+    B, n_kv, qg = 1, 8, 64
+    n_kv = n_kv if n_q > 16 else 2
+    q = rows_f64(L, (B, n_q * HD), torch.bfloat16, spread=0.3)
+    kd, vd = (d(c) for c in make_cache(L, B, L, n_kv, qg, hm))
+    mask = np.ones((B, n_q), np.uint8)
+    mask[0, 3] = 0
+    clean = run_attention(q.cuda(), kd, vd, d(mask), n_q, n_kv, HD, qg, None, hm)
+    assert torch.isfinite(clean).all()
+    for at, value in ((1, float("inf")), (1, float("-inf")), (1, float("nan")), (3, float("nan")), (n_q - 1, float("inf"))):
+        say("queries", n_q, L, hm, at, value)
+        x = q.clone()
+        x[0, at * HD + 77] = value
+        o = run_attention(x.cuda(), kd, vd, d(mask), n_q, n_kv, HD, qg, None, hm)
+        head = slice(at * HD, (at + 1) * HD)
+        if mask[0, at]:
+            assert torch.isnan(o[0, head]).all()
+            o[0, head] = clean[0, head]
+        assert torch.equal(o.view(torch.int16), clean.view(torch.int16))
+
+
 def test_cache_beyond_32_bit_offsets():
     """Rows more than 4 GiB into a cache: written, read back and attended to."""
     n_kv, qg, L = 32, 32, 1 << 20

@@ -97,6 +97,11 @@ def test_rows_validation(read, kw, status, msg):
     assert msg in err()
 
 
+def test_rows_need_two_buffers():
+    assert quantize(vc=A) == W.ERR_INVALID_ARG and "k_cache and v_cache are the same" in err()
+    assert quantize(read=True, v=A) == W.ERR_INVALID_ARG and "k and v are the same" in err()
+
+
 def test_rows_empty_calls():
     for read in (False, True):
         for kw in (dict(n_seq=0), dict(T=0)):
