@@ -36,6 +36,13 @@
 //           with exponent 2^4 and the code in its top mantissa bits: a shift and
 //           an and-or make two.  Row (h, g) of nibble n counts where g = n mod 4.
 // The low terms of P.V are fp32 sums per (head, group) beside it.
+//
+// Bound by the cache's bytes (32 x 8192 keys, 8 KV heads, groups of 32, head-major:
+// 336 MB in 67 us with its join, 5.0 TB/s; 64 ragged ones of up to 32768, groups of
+// 64: 1.2 GB in 223, 5.4; a pure read of the same shape 6.1), short calls by latency
+// (500 keys: 6.3 us).  A tile is 175 vector instructions; two in flight a wave
+// (three or four, or two computed together, cost 1-2 us a call in code and in loads
+// past the end).
 #include <algorithm>
 
 #include "common.h"
@@ -966,7 +973,10 @@ hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStrea
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.table) return e;
   const int heads = a.B * a.n_q, per = (a.wgs ? 8 * a.wgs : a.waves) / pairs;  // segments a pair, nothing masked
-  if (per > 32)
+  // (lanes of segments 2, 8, 32, whole call in us: 8192 keys, 8 KV heads, 1 sequence
+  // (256 segments) 23.4, 13.8, 12.6; 4 (64) 21.6, 17.1, 17.4; 8 (32) 24.4, 22.7, 23.7;
+  // 32 (8) 68.3, 68.5, 74.8)
+  if (per > 64)
     WIDE_LAUNCH_NAMED("wide_attn_decode_kvq_merge", wide_attn_decode_kvq_merge<32>, dim3(heads), dim3(1024), 0, s, a);
   else if (per > 8)
     WIDE_LAUNCH_NAMED("wide_attn_decode_kvq_merge", wide_attn_decode_kvq_merge<8>, dim3(heads), dim3(256), 0, s, a);
