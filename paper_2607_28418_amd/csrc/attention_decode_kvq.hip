@@ -483,14 +483,21 @@ __global__ __launch_bounds__(NW * 64, 2) void wide_attn_decode_kvq(AttnDecArgs a
   const int nw = min(NW, (len + kTile - 1) / kTile);  // waves that had a tile
   for (int i = threadIdx.x; i < a.qpk * 64; i += NW * 64) {
     const int h = i >> 6, d = 2 * (i & 63);
-    float mm = -INFINITY;
-    for (int k = 0; k < nw; ++k) mm = fmaxf(mm, s_m[k][h]);
-    float zz = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int k = 0; k < nw; ++k) {
-      const float f = __builtin_amdgcn_exp2f(s_m[k][h] - mm);
-      zz = fmaf(f, s_z[k][h], zz);
-      o0 = fmaf(f, s_o[k][h][d], o0);
-      o1 = fmaf(f, s_o[k][h][d + 1], o1);
+    float mk[NW], mm = -INFINITY, zz = 0.0f, o0 = 0.0f, o1 = 0.0f;
+    float2 ok[NW];
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {  // (all of them: the reads go together; the first wave's for those without)
+      const int kk = k < nw ? k : 0;
+      mk[k] = k < nw ? s_m[kk][h] : -INFINITY;
+      ok[k] = *reinterpret_cast<const float2*>(&s_o[kk][h][d]);
+      mm = fmaxf(mm, mk[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      const float f = k < nw ? __builtin_amdgcn_exp2f(mk[k] - mm) : 0.0f;
+      zz = fmaf(f, s_z[k < nw ? k : 0][h], zz);
+      o0 = fmaf(f, ok[k].x, o0);
+      o1 = fmaf(f, ok[k].y, o1);
     }
     const float inv = 1.0f / zz;
     out[i] = (act >> h) & 1u ? pack_bf16x2_hw(o0 * inv, o1 * inv) : 0u;
@@ -886,19 +893,29 @@ __global__ __launch_bounds__(SL == 2 ? 256 : SL * 32) void wide_attn_decode_kvq_
     }
     *reinterpret_cast<f32x4*>(&s_o[sl][4 * dq]) = o;
     __syncthreads();
-    if (sl != 0) return;
-    const int n = min(SL, nseg);  // lanes that had a segment
-    float mn = s_m[0];
-    for (int k = 1; k < n; ++k) mn = fmaxf(mn, s_m[k]);
-    z = 0.0f;
-    o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int k = 0; k < n; ++k) {
-      const float f = __builtin_amdgcn_exp2f(s_m[k] - mn);
-      const f32x4 v = *reinterpret_cast<const f32x4*>(&s_o[k][4 * dq]);
-      z = fmaf(f, s_z[k], z);
+    if (t >= 64) return;
+    // one wave: the lanes' weights, then four dimensions a lane over half of the lanes of segments each
+    const int k = t % SL;  // (a lane without a segment: maximum -inf, sums 0)
+    const float mk = s_m[k];
+    float mn = mk;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(f, v[e], o[e]);
+    for (int d = SL / 2; d >= 1; d >>= 1) mn = fmaxf(mn, __shfl_xor(mn, d));
+    const float f = mk == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mk - mn);
+    z = f * s_z[k];
+#pragma unroll
+    for (int d = SL / 2; d >= 1; d >>= 1) z += __shfl_xor(z, d);
+    o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < SL / 2; ++i) {
+      const int l = 2 * i + sl;
+      const float fl = __shfl(f, l);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(&s_o[l][4 * dq]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(fl, v[e], o[e]);
     }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], 32);
+    if (sl != 0) return;
   }
   const float inv = 1.0f / z;
   *reinterpret_cast<uint64_t*>(out) =
@@ -974,8 +991,8 @@ hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStrea
   if (e != hipSuccess || !a.table) return e;
   const int heads = a.B * a.n_q, per = (a.wgs ? 8 * a.wgs : a.waves) / pairs;  // segments a pair, nothing masked
   // (lanes of segments 2, 8, 32, whole call in us: 8192 keys, 8 KV heads, 1 sequence
-  // (256 segments) 23.4, 13.8, 12.6; 4 (64) 21.6, 17.1, 17.4; 8 (32) 24.4, 22.7, 23.7;
-  // 32 (8) 68.3, 68.5, 74.8)
+  // (256 segments) 23.1, 13.2, 11.7; 2 (128) 26.2, 15.9, 14.5; 4 (64) 21.6, 16.7, 16.7;
+  // 8 (32) 24.3, 22.3, 23.0; 32 (8) 68.5, 68.4, 73.7)
   if (per > 64)
     WIDE_LAUNCH_NAMED("wide_attn_decode_kvq_merge", wide_attn_decode_kvq_merge<32>, dim3(heads), dim3(1024), 0, s, a);
   else if (per > 8)
