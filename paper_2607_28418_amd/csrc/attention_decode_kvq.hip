@@ -179,7 +179,8 @@ struct Attend {
         const float x = g4 & 1 ? low : s;
         return u32x2{pk(slot == 0 ? x : 0.0f, slot == 1 ? x : 0.0f), pk(slot == 2 ? x : 0.0f, slot == 3 ? x : 0.0f)};
       } else if constexpr (NG == 2) {
-        return u32x2{pk(slot == 0 ? s : 0.0f, slot == 1 ? s : 0.0f), pk(slot == 0 ? low : 0.0f, slot == 1 ? low : 0.0f)};
+        return u32x2{pk(slot == 0 ? s : 0.0f, slot == 1 ? s : 0.0f),
+                     pk(slot == 0 ? low : 0.0f, slot == 1 ? low : 0.0f)};
       } else {
         return u32x2{pk(s, low), 0u};
       }
@@ -347,7 +348,8 @@ struct Attend {
         for (int r = 0; r < 4; ++r) rest[r] = ps[r] - __uint_as_float(__float_as_uint(ps[r]) & 0xffff0000u);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          P1[s][2 * t + i] = __builtin_amdgcn_perm(__float_as_uint(ps[2 * i + 1]), __float_as_uint(ps[2 * i]), 0x07060302u);
+          P1[s][2 * t + i] =
+              __builtin_amdgcn_perm(__float_as_uint(ps[2 * i + 1]), __float_as_uint(ps[2 * i]), 0x07060302u);
           P2[s][2 * t + i] = pack_bf16x2_hw(rest[2 * i], rest[2 * i + 1]);
         }
       }
@@ -581,19 +583,20 @@ struct RowStage {
 
 typedef void __attribute__((address_space(3)))* lds_t;
 
-// Registers of a wave's tile from the stage `at` bytes into the ring.  Each group of reads is one
-// asm block with its wait: before a plain LDS read the compiler waits for every
-// direct-to-LDS load under way.
+// Registers of a wave's tile from the stage `at` bytes into the ring.  Each group
+// of reads is one asm block with its wait: before a plain LDS read the compiler
+// waits for every direct-to-LDS load under way.
 template <int NG>
-__device__ __forceinline__ void fetch(uint32_t at, const uint32_t (&k_at)[2], const uint32_t (&km_at)[2], const uint32_t (&vm_at)[2],
-                                      const uint32_t (&v_at)[2][4], Tile<NG>& T) {
+__device__ __forceinline__ void fetch(uint32_t at, const uint32_t (&k_at)[2], const uint32_t (&km_at)[2],
+                                      const uint32_t (&vm_at)[2], const uint32_t (&v_at)[2][4], Tile<NG>& T) {
   if constexpr (NG == 4) {
     asm volatile(
         "ds_read_b128 %0, %6\n\tds_read_b128 %1, %7\n\tds_read_b64 %2, %8\n\t"
         "ds_read_b64 %3, %9\n\tds_read_b64 %4, %10\n\tds_read_b64 %5, %11\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(T.kc[0]), "=&v"(T.kc[1]), "=&v"(T.km[0]), "=&v"(T.km[1]), "=&v"(T.vm[0]), "=&v"(T.vm[1])
-        : "v"(k_at[0] + at), "v"(k_at[1] + at), "v"(km_at[0] + at), "v"(km_at[1] + at), "v"(vm_at[0] + at), "v"(vm_at[1] + at)
+        : "v"(k_at[0] + at), "v"(k_at[1] + at), "v"(km_at[0] + at), "v"(km_at[1] + at), "v"(vm_at[0] + at),
+          "v"(vm_at[1] + at)
         : "memory");
   } else if constexpr (NG == 2) {
     u32x2 k[2][2];
@@ -603,7 +606,8 @@ __device__ __forceinline__ void fetch(uint32_t at, const uint32_t (&k_at)[2], co
         "ds_read_b64 %6, %12\n\tds_read_b64 %7, %13\n\ts_waitcnt lgkmcnt(0)"
         : "=&v"(k[0][0]), "=&v"(k[0][1]), "=&v"(k[1][0]), "=&v"(k[1][1]), "=&v"(T.km[0]), "=&v"(T.km[1]),
           "=&v"(T.vm[0]), "=&v"(T.vm[1])
-        : "v"(k_at[0] + at), "v"(k_at[1] + at), "v"(km_at[0] + at), "v"(km_at[1] + at), "v"(vm_at[0] + at), "v"(vm_at[1] + at)
+        : "v"(k_at[0] + at), "v"(k_at[1] + at), "v"(km_at[0] + at), "v"(km_at[1] + at), "v"(vm_at[0] + at),
+          "v"(vm_at[1] + at)
         : "memory");
 #pragma unroll
     for (int t = 0; t < 2; ++t) T.kc[t] = u32x4{k[t][0][0], k[t][0][1], k[t][1][0], k[t][1][1]};
@@ -630,8 +634,8 @@ __device__ __forceinline__ void fetch(uint32_t at, const uint32_t (&k_at)[2], co
       "ds_read_b32 %3, %11\n\tds_read_b32 %4, %12\n\tds_read_b32 %5, %13\n\t"
       "ds_read_b32 %6, %14\n\tds_read_b32 %7, %15\n\ts_waitcnt lgkmcnt(0)"
       : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
-      : "v"(v_at[0][0] + at), "v"(v_at[0][1] + at), "v"(v_at[0][2] + at), "v"(v_at[0][3] + at), "v"(v_at[1][0] + at), "v"(v_at[1][1] + at),
-        "v"(v_at[1][2] + at), "v"(v_at[1][3] + at)
+      : "v"(v_at[0][0] + at), "v"(v_at[0][1] + at), "v"(v_at[0][2] + at), "v"(v_at[0][3] + at),
+        "v"(v_at[1][0] + at), "v"(v_at[1][1] + at), "v"(v_at[1][2] + at), "v"(v_at[1][3] + at)
       : "memory");
 #pragma unroll
   for (int t = 0; t < 2; ++t)
@@ -777,7 +781,8 @@ __global__ __launch_bounds__(512, 2) void wide_attn_decode_kvq_rows(AttnDecArgs 
 #pragma unroll
     for (int k = 0; k < St::LOADS; ++k)
       if (kWave * (k + 1) <= St::CW || kWave * k + lane < St::CW)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(view, (lds_t)(dst + st * St::SIZE + 1024 * k), 16, (int)off[k], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(view, (lds_t)(dst + st * St::SIZE + 1024 * k), 16, (int)off[k], 0, 0,
+                                                 0);
   };
   load(j, 0);
   load(j + ks, 1);

@@ -309,7 +309,8 @@ hipError_t launch_kv_quant(KvqArgs a, bool f32, bool read, hipStream_t s) {
   if (tokens == 0) return hipSuccess;
   a.by_heads = fast_div((uint32_t)a.n_kv);
   a.by_T = fast_div((uint32_t)a.T);
-  a.blocks = (uint32_t)(a.head_major ? (tokens + kQRows - 1) / kQRows * a.n_kv : (tokens * a.n_kv + kQRows - 1) / kQRows);
+  a.blocks = (uint32_t)(a.head_major ? (tokens + kQRows - 1) / kQRows * a.n_kv
+                                     : (tokens * a.n_kv + kQRows - 1) / kQRows);
   const dim3 grid(std::min(a.blocks, 1u << 22), 2);
 #define WIDE_KVQ(T, NG, HM)                                                                               \
   do {                                                                                                    \
