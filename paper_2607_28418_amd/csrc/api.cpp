@@ -1496,7 +1496,7 @@ wide_status_t wide_attention_decode_kvq(wide_dtype_t dt, int64_t batch, int32_t 
   CHECK(check_ptr(v_cache, "v_cache"));
   CHECK(check_ptr(o, "o"));
   const bool head_major = kv_layout == WIDE_KV_HEAD_MAJOR || n_kv_heads == 1;  // (the same rows)
-  const bool whole = (size_t)n_kv_heads * wide_kv_quant_row_bytes(head_dim, quant_group) % 16 == 0;
+  const bool whole = wide::kvq_group_heads(n_kv_heads) * wide_kv_quant_row_bytes(head_dim, quant_group) % 16 == 0;
   const wide::KvqPlan plan = wide::attn_decode_kvq_plan(batch, n_kv_heads, L, s.qpk, head_major, whole);
   KvqWS w;
   {

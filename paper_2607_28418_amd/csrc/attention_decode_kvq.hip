@@ -548,11 +548,12 @@ __global__ __launch_bounds__(kSplitThreads, 2) void wide_attn_decode_kvq_runs(At
 // a line each, so heads read one by one, 1.6 lines for 80 bytes, get little more
 // than half of the rate (32 x 8192 keys, 8 KV heads: 98 us; 122 with the heads of a
 // position on different XCDs, too, so that each fetches the line).  Here a
-// workgroup of eight waves reads whole runs of rows for eight heads into LDS (75 us).
+// workgroup of eight waves reads whole runs of rows for eight heads into LDS (75 us),
+// or for four or two, the largest number that divides the heads.
 //
 // A unit of work is (sequence, eight KV heads, run of stages); a stage is 256 rows:
-// 32 positions of eight heads, 64 of four, 128 of two.  Eight rows in a row are a
-// super-row, 8 R bytes; wave w of the first four loads super-rows 8 w .. 8 w + 7 of
+// 32 positions of eight heads, 64 of four, 128 of two.  Eight rows (of one, two or
+// four positions) are a super-row, 8 R bytes; wave w of the first four loads super-rows 8 w .. 8 w + 7 of
 // K, the others of V, in 16-byte chunks, direct to LDS, two stages ahead, leaving
 // out chunks of inactive heads; then wave w attends for head w mod heads over the
 // 32 positions of part w / heads.  The units of a sequence take q stages each, the
@@ -664,7 +665,7 @@ __global__ __launch_bounds__(512, 2) void wide_attn_decode_kvq_rows(AttnDecArgs 
   __shared__ int s_cnt[NW][kWave];
   extern __shared__ HeadGroup s_grp[];
   const int tid = threadIdx.x, w = wave_id(), lane = lane_id();
-  const int hg = min(a.n_kv, 8), per_seq = a.n_kv / hg, groups = a.B * per_seq;  // heads of a group, groups
+  const int hg = kvq_group_heads(a.n_kv), per_seq = a.n_kv / hg, groups = a.B * per_seq;  // heads of a group, groups
   const int ks = 256 / hg;                                                      // positions of a stage
 
   // ---- the groups' active heads and stages
@@ -765,6 +766,7 @@ __global__ __launch_bounds__(512, 2) void wide_attn_decode_kvq_rows(AttnDecArgs 
   // ---- loads
   const int64_t ld = (int64_t)a.n_kv * R;
   const char* base = reinterpret_cast<const char*>(w < 4 ? a.k : a.v) + ((int64_t)b * a.L * a.n_kv + head0) * R;
+  const int per_pos = hg * R / 16;  // chunks of a position
   uint32_t off[St::LOADS];
 #pragma unroll
   for (int k = 0; k < St::LOADS; ++k) {
@@ -772,7 +774,8 @@ __global__ __launch_bounds__(512, 2) void wide_attn_decode_kvq_rows(AttnDecArgs 
     int ch = e % St::CK + St::turn(sr);
     ch = ch >= St::CK ? ch - St::CK : ch;
     const uint32_t heads = 1u << (16 * ch / R & (hg - 1)) | 1u << ((16 * ch + 15) / R & (hg - 1));
-    off[k] = act & heads ? (uint32_t)(sr * (hg == 8 ? (int)ld : St::SUPER) + 16 * ch) : kOffNone;
+    const int pos = (ch >= per_pos) + (ch >= 2 * per_pos) + (ch >= 3 * per_pos);  // of the super-row's 8 / hg
+    off[k] = act & heads ? (uint32_t)((sr * (8 / hg) + pos) * (int)ld + 16 * (ch - pos * per_pos)) : kOffNone;
   }
   char* dst = s_ring + (w < 4 ? 0 : St::D * St::SIZE) + (w & 3) * St::CW * 16;
   auto load = [&](int j, int st) {
@@ -937,21 +940,22 @@ constexpr int kMany = 512;   // pairs
 //  - contexts of up to 64 tiles: a workgroup per pair.  One sequence of 1500 keys,
 //    8 KV heads: 10 against 11 as runs, of 3000: 16 against 12; 64 of 1024: 16
 //    against 22; token-major 32 of 2048: 22, as rows 27;
-//  - token-major, more than four stages of rows a workgroup: rows.  16 sequences
-//    of 4096 (eight stages): 25 against 35 as runs, 48 a workgroup per pair for 32
-//    of them (43); 8 of 4096 (four): 20 and 18.  With more than 512 groups each
-//    workgroup spends too long on the list: 900 sequences of 2100 682, a workgroup
-//    per pair 616; 600 of them 393 and 411;
+//  - token-major, an even number of KV heads (whole 16-byte pieces), more than four
+//    stages of rows a workgroup: rows.  16 sequences of 4096, 8 KV heads (eight
+//    stages): 25 against 35 as runs, 48 a workgroup per pair for 32 of them (43); 8
+//    of 4096 (four): 20 and 18; 32 of 8192, 12 KV heads: 112, 185, 147; 10: 115, 153,
+//    138.  With more than 512 groups each workgroup spends too long on the list: 900
+//    sequences of 2100 682, a workgroup per pair 616; 600 of them 393 and 411;
 //  - other token-major caches of more than 512 pairs: a workgroup per pair, whose
 //    neighbours read the same lines at about the same time (200 sequences of 4096,
-//    3 KV heads: 108, as runs 146; but 32 ragged ones of up to 8192, 12 KV heads, half
-//    of them masked: 80 and 55);
+//    3 KV heads: 108, as runs 146);
 //  - else runs.
 KvqPlan attn_decode_kvq_plan(int64_t B, int n_kv, int L, int qpk, bool head_major, bool whole) {
   KvqPlan p{};
-  const int64_t pairs = B * n_kv, tiles = (L + kTile - 1) / kTile, groups = pairs / std::min(n_kv, 8);
+  const int hg = kvq_group_heads(n_kv);
+  const int64_t pairs = B * n_kv, tiles = (L + kTile - 1) / kTile, groups = pairs / hg;
   if (tiles <= kShort || pairs * tiles > 0x7fffffff) return p;
-  if (!head_major && whole && (n_kv % 8 == 0 || n_kv == 4 || n_kv == 2) && tiles * pairs / 8 > kStages * kKvqWgs) {
+  if (!head_major && whole && hg > 1 && tiles * pairs / 8 > kStages * kKvqWgs) {
     if (groups > kKvqMaxGroups) return p;
     // at least two workgroups a group, whole rounds of them
     p.wgs = (int)std::max<int64_t>(kKvqWgs, (2 * groups + kKvqWgs - 1) / kKvqWgs * kKvqWgs);
@@ -967,7 +971,7 @@ KvqPlan attn_decode_kvq_plan(int64_t B, int n_kv, int L, int qpk, bool head_majo
 
 hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStream_t s) {
   if (a.B == 0) return hipSuccess;
-  const int pairs = a.B * a.n_kv, lds = (pairs + 1) * (int)sizeof(uint64_t), groups = pairs / std::min(a.n_kv, 8);
+  const int pairs = a.B * a.n_kv, lds = (pairs + 1) * (int)sizeof(uint64_t), groups = pairs / kvq_group_heads(a.n_kv);
 #define WIDE_DEC4(NG, H)                                                                                     \
   do {                                                                                                       \
     constexpr int NW = 8;                                                                                    \

@@ -315,11 +315,16 @@ hipError_t launch_kv_quant(KvqArgs a, bool f32, bool read, hipStream_t s);
 // Decode attention; a.k and a.v are the 4-bit caches, quant_groups per row 1, 2
 // or 4.  What its waves (workgroups) that share the work take of the workspace,
 // in a.table and a.part; neither: one workgroup per pair, no workspace.  whole:
-// a position's rows are a multiple of 16 bytes.
+// the rows of a position's kvq_group_heads are a multiple of 16 bytes.
 constexpr int kKvqMaxPairs = 8000;   // listed in LDS, two workgroups a CU
 constexpr int kKvqMaxGroups = 512;   // of up to eight KV heads of a sequence, listed beside their rows
 constexpr int kKvqMinTiles = 2;      // 64 keys: the shortest run of a wave
 constexpr int kKvqWgs = 256;         // one a CU
+// KV heads whose rows a workgroup reads together: 8, 4, 2 or 1.
+__host__ __device__ inline int kvq_group_heads(int n_kv) {
+  const int low = n_kv & -n_kv;
+  return low < 8 ? low : 8;
+}
 struct KvqPlan {
   int waves, wgs;
   size_t table_ints, part_floats;

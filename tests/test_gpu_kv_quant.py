@@ -306,6 +306,9 @@ def test_attention_batches(B, L, n_q, n_kv, group, qg, hm, ragged):
     (9, 2100, 16, 16, 128, "random"),          # two sets of eight
     (33, 2081, 12, 4, 384, "random"),
     (64, 2081, 32, 2, 256, "random"),
+    (22, 2081, 24, 12, 256, "random"),         # three sets of four
+    (26, 2081, 20, 10, 256, "random"),         # five of two
+    (40, 2081, 10, 5, 128, "random"),          # one by one
     (1, 33000, 8, 8, 128, None),
     (300, 2049, 8, 8, 128, "random"),          # more groups than workgroups
 ])
