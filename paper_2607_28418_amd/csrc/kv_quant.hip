@@ -25,7 +25,8 @@
 // quantising by the vector ALUs: 210 instructions a lane, 11 of the 13 us that 8192
 // positions of 8 heads take in bf16 (44 MB, 3.3 TB/s).  Exact decisions are five
 // fp32 operations an element where every x - low is exact (nearly always, in bf16;
-// all of it in fp64 took 22 us), fp64 elsewhere.
+// all of it in fp64 took 22 us), fp64 and what its differences lose elsewhere.  fp32
+// rows take the fp64 arm: the same positions (78 MB) 18 us.
 #include <algorithm>
 
 #include "common.h"
@@ -96,14 +97,21 @@ __device__ __forceinline__ uint32_t row_ror(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x120 + N, 0xF, 0xF, true);
 }
 
-// (greatest - low) / 15 to the nearest bf16, ties to even, in one rounding;
-// 0 below 2^-126.  The fp64 quotient is never a tie that the exact one is not:
+// a - b = d + this, exactly (d the rounded difference; Knuth's two-sum).
+__device__ __forceinline__ double diff_rest(double a, double b, double d) {
+  const double v = a - d;
+  return (a - (d + v)) + (v - b);
+}
+
+// (w + rest) / 15 to the nearest bf16, ties to even, in one rounding; 0 below
+// 2^-126.  The fp64 quotient w / 15 is never a tie that the exact one is not:
 // a 53-bit w differs from 15 t by at least ulp(w), more than 15/16 of it is
-// more than half an ulp of the quotient.
-__device__ __forceinline__ float group_scale(double w) {
+// more than half an ulp of the quotient.  rest, half an ulp of w at most, counts
+// where w is such a 15 t.
+__device__ __forceinline__ float group_scale(double w, double rest) {
   const double q = w / 15.0;
   uint64_t u = __double_as_longlong(q);
-  u += ((1ull << 44) - 1) + ((u >> 45) & 1);
+  u += ((1ull << 44) - 1) + (rest == 0.0 ? (u >> 45) & 1 : rest > 0.0);
   const double s = __longlong_as_double(u & ~((1ull << 45) - 1));
   return s < 0x1p-126 ? 0.0f : (float)s;
 }
@@ -114,7 +122,8 @@ struct Coded {
   uint32_t scale, low, code[4];
 };
 
-// Every step in fp64 where a rounding could change a decision.
+// Every step in fp64 where a rounding could change a decision, and what a
+// difference of values 2^45 apart loses there.
 template <bool CUT>
 __device__ __forceinline__ Coded code_fp64(const float (&x)[8], float lo, float hi, bool bad) {
   uint32_t lbits = __float_as_uint(lo);
@@ -123,18 +132,25 @@ __device__ __forceinline__ Coded code_fp64(const float (&x)[8], float lo, float 
     lbits = (lbits >> 31) && cut != lbits ? cut + 0x10000u : cut;
   }
   const double low = (double)__uint_as_float(lbits);
-  const float s = bad ? 0.0f : group_scale((double)hi - low);
+  const double w = (double)hi - low;
+  const float s = bad ? 0.0f : group_scale(w, diff_rest(hi, low, w));
   const float inv = s > 0.0f ? 1.0f / s : 0.0f, lf = __uint_as_float(lbits);
   const double sd = (double)s, half = 0.5 * sd;
   uint32_t code[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    // the nearest code up to fp32 rounding, then the exact remainder decides
+    // the nearest code up to fp32 rounding, then the remainder decides.  The
+    // difference d, and so the remainder, may lack half an ulp of d, which counts
+    // on the border only: d is at most 16 s, so both sides of the comparison are
+    // multiples of that ulp.
     float kf = rintf((x[e] - lf) * inv);
     kf = s > 0.0f ? fminf(fmaxf(kf, 0.0f), 15.0f) : 0.0f;
-    const double rem = fma(-sd, (double)kf, (double)x[e] - low);
+    const double d = (double)x[e] - low, rem = fma(-sd, (double)kf, d);
     int c = (int)kf;
-    if (s > 0.0f && (fabs(rem) > half || (fabs(rem) == half && (c & 1)))) c += rem > 0.0 ? 1 : -1;
+    if (s > 0.0f && fabs(rem) >= half) {
+      const double rest = diff_rest(x[e], low, d);
+      if (fabs(rem) > half || (rest == 0.0 ? (c & 1) != 0 : (rest > 0.0) == (rem > 0.0))) c += rem > 0.0 ? 1 : -1;
+    }
     code[e] = (uint32_t)min(max(c, 0), 15);
   }
   Coded o;

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2607_28418_amd as W
-from tests import _kvq
+from tests import _kvq, _kvq_exact
 
 pytestmark = pytest.mark.gpu
 HD = 128
@@ -145,6 +145,19 @@ def test_quantize_borders(qg, spread):
         W.wide_kv_quantize(t.cuda(), -t.cuda(), kc, vc, 1, HD, qg)
         assert np.array_equal(kc.cpu().numpy()[0, :, 0], _kvq.quantize(x, qg))
         assert np.array_equal(vc.cpu().numpy()[0, :, 0], _kvq.quantize(-x, qg))
+
+
+@pytest.mark.parametrize("qg", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_quantize_far_apart(dtype, qg):
+    """Values and ranges off a border by less than an fp64 difference holds, against whole numbers."""
+    x = _kvq_exact.border_rows()[dtype == torch.float32]
+    t = torch.from_numpy(x).to(dtype)
+    kc = torch.zeros(1, len(x), 1, _kvq.row_bytes(qg), dtype=torch.uint8, device="cuda")
+    vc = kc.clone()
+    W.wide_kv_quantize(t.cuda(), -t.cuda(), kc, vc, 1, HD, qg)
+    assert np.array_equal(kc.cpu().numpy()[0, :, 0], _kvq_exact.quantize(x, qg))
+    assert np.array_equal(vc.cpu().numpy()[0, :, 0], _kvq_exact.quantize(-x, qg))
 
 
 # ---- reading back ------------------------------------------------------------------

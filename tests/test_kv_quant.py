@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import paper_2607_28418_amd as W
-from tests import _kvq
+from tests import _kvq, _kvq_exact
 
 A = ctypes.c_void_p(0x10000)
 MIS = ctypes.c_void_p(0x10008)
@@ -61,6 +61,26 @@ def test_plain_rows_not_finite():
 def test_positions():
     assert _kvq.where_rows(2, 3, 4, [-1, 2], [2, 9]) == [(1, 0, 0), (2, 0, 1), (3, 1, 2), (4, 1, 3)]
     assert _kvq.where_rows(1, 2, 4, None, None) == [(0, 0, 0), (1, 0, 1)]
+
+
+def test_exact_rows():
+    x = np.full((2, 128), 2.0 ** -60)
+    x[:, 0], x[:, 1] = -1.0, 29.0           # low -1, scale 2: 2^-60 lies just above the border of codes 0 and 1
+    x[1] = -x[1]                            # low -29: -2^-60 just below the border of 14 and 15
+    s, low, c = _kvq.parts(_kvq_exact.quantize(x, 32), 32)
+    assert (s[:, :32] == 2).all() and low[0, 0] == -1 and low[1, 0] == -29
+    assert c[0, :32].tolist() == [0, 15] + [1] * 30 and c[1, :32].tolist() == [15, 0] + [14] * 30
+    assert (s[:, 32:] == 0).all() and (low[0, 32:] == 2.0 ** -60).all() and (low[1, 32:] == -2.0 ** -60).all()
+    g = np.random.default_rng(3)            # where 53 bits are enough, the rows of the plain form
+    y = g.normal(size=(200, 128)).astype(np.float32).astype(np.float64)
+    y[100:] = g.integers(-40, 41, (100, 128)) * 2.0 ** -g.integers(0, 20, (100, 128))
+    y[:5, 3] = np.nan, np.inf, 2.0 ** 127, 2.0 ** -140, -2.0 ** -149
+    y[6] = 2.0 ** -133 * (np.arange(128) % 7)
+    for qg in (32, 64, 128):
+        assert np.array_equal(_kvq_exact.quantize(y, qg), _kvq.quantize(y, qg))
+    few, all_ = _kvq_exact.border_rows()
+    assert (torch.from_numpy(few).bfloat16().double().numpy() == few).all()
+    assert (torch.from_numpy(all_).float().double().numpy() == all_).all()
 
 
 # ---- refusals ------------------------------------------------------------------------
