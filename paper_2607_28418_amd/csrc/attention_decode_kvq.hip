@@ -932,6 +932,7 @@ __global__ __launch_bounds__(SL == 2 ? 256 : SL * 32) void wide_attn_decode_kvq_
 
 }  // namespace
 
+constexpr int kLaunchPairs = 1 << 22;  // a workgroup each: a launch has fewer than 2^32 threads
 constexpr int kShort = 64;   // tiles
 constexpr int kStages = 4;   // of a workgroup
 constexpr int kMany = 512;   // pairs
@@ -971,6 +972,23 @@ KvqPlan attn_decode_kvq_plan(int64_t B, int n_kv, int L, int qpk, bool head_majo
 
 hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStream_t s) {
   if (a.B == 0) return hipSuccess;
+  const int slice = kLaunchPairs / a.n_kv;  // sequences (n_kv is at most 2^16)
+  if (!a.table && a.B > slice) {
+    const int64_t seq = (int64_t)a.L * a.n_kv * (64 + 4 * quant_groups) / (int64_t)sizeof *a.k;
+    for (int64_t b = 0; b < a.B; b += slice) {
+      AttnDecArgs part = a;
+      part.B = (int)std::min<int64_t>(slice, a.B - b);
+      part.q += b * a.n_q * 128;
+      part.o += b * a.n_q * 128;
+      part.k += b * seq;
+      part.v += b * seq;
+      part.mask += b * a.ng;
+      if (a.kv_len) part.kv_len += b;
+      const hipError_t e = launch_attention_decode_kvq(part, quant_groups, s);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
   const int pairs = a.B * a.n_kv, lds = (pairs + 1) * (int)sizeof(uint64_t), groups = pairs / kvq_group_heads(a.n_kv);
 #define WIDE_DEC4(NG, H)                                                                                     \
   do {                                                                                                       \

@@ -372,6 +372,35 @@ def test_attention_many_sequences(B, hm):
     assert not o.cpu()[torch.from_numpy(off)].any() and torch.isfinite(o).all()
 
 
+@pytest.mark.parametrize("n_kv,hm", [(8, True), (9, False)])
+def test_attention_more_pairs_than_a_launch_holds(n_kv, hm):
+    """2^23 and more (sequence, KV head) pairs: more threads than one launch takes.  With one key the
+    answer is its value, with none zeros."""
+    B, L, qg = (1 << 23) // n_kv + 5, 1, 128
+    say("pairs", B * n_kv, hm)
+    g = torch.Generator(device="cuda").manual_seed(n_kv)
+    kv = torch.randn((B, n_kv * HD), generator=g, device="cuda").bfloat16()
+    kc = torch.zeros(cache_shape(B, L, n_kv, qg, hm), dtype=torch.uint8, device="cuda")
+    vc = torch.zeros_like(kc)
+    W.wide_kv_quantize(kv, kv, kc, vc, n_kv, HD, qg, head_major=hm)
+    mask = (torch.rand((B, n_kv), generator=g, device="cuda") < 0.9).to(torch.uint8)
+    kv_len = (torch.rand((B,), generator=g, device="cuda") < 0.9).int()
+    o = run_attention(kv, kc, vc, mask, n_kv, n_kv, HD, qg, kv_len, hm)
+    n = 0
+    for at in torch.arange(B, device="cuda").split(1 << 17):
+        v = W.wide_kv_dequantize(kc[at[0]:at[-1] + 1], vc[at[0]:at[-1] + 1], 1, n_kv, HD, qg, head_major=hm,
+                                 dtype=torch.float32)[1].view(-1, n_kv, HD)
+        on = (mask[at] != 0) & (kv_len[at] > 0)[:, None]
+        got = o[at].view(-1, n_kv, HD).float()
+        # p = 1; p s in two bf16 parts (2^-16) over 16 + c and 16 s off again, fp32, one rounding to bf16: with
+        # v from low to low + 15 s and low < 0 < low + 15 s (normal values), 47 s + |low| <= 5 (|low| + |high|)
+        size = 5 * (v.amax(-1, keepdim=True).abs() + v.amin(-1, keepdim=True).abs())
+        tol = 2.0 ** -8 * v.abs() + size * (2.0 ** -16 + 70 * 2.0 ** -24)
+        assert ((got - v).abs() <= tol)[on].all() and not got[~on].any()
+        n += int(on.sum())
+    assert n > B * n_kv // 2
+
+
 @pytest.mark.parametrize("L,hm", [(300, False), (3000, True), (33000, False)])
 @pytest.mark.parametrize("n_q", [8, 16, 32])
 def test_attention_not_finite_queries(n_q, L, hm):
