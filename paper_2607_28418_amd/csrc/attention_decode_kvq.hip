@@ -994,10 +994,10 @@ hipError_t launch_attention_decode_kvq(AttnDecArgs a, int quant_groups, hipStrea
   do {                                                                                                       \
     constexpr int NW = 8;                                                                                    \
     if (a.wgs)                                                                                               \
-      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_rows<NG, H>), dim3(a.wgs), dim3(512),  \
+      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq/rows", (wide_attn_decode_kvq_rows<NG, H>), dim3(a.wgs), dim3(512), \
                         groups * (int)sizeof(HeadGroup), s, a);                                              \
     else if (a.table)                                                                                        \
-      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq_runs<NG, H>), dim3(a.waves / 4),      \
+      WIDE_LAUNCH_NAMED("wide_attn_decode_kvq/runs", (wide_attn_decode_kvq_runs<NG, H>), dim3(a.waves / 4), \
                         dim3(kSplitThreads), lds, s, a);                                                     \
     else                                                                                                     \
       WIDE_LAUNCH_NAMED("wide_attn_decode_kvq", (wide_attn_decode_kvq<NG, H, NW>), dim3(pairs), dim3(NW * 64), \

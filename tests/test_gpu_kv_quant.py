@@ -372,6 +372,59 @@ def test_attention_many_sequences(B, hm):
     assert not o.cpu()[torch.from_numpy(off)].any() and torch.isfinite(o).all()
 
 
+def kernels_of(call):
+    """Launches of a call's attention kernels: (a workgroup per pair, equal runs, whole rows, joins)."""
+    W.wide_timing_enable(True)
+    W.wide_timing_reset()
+    try:
+        call()
+        every, runs, rows, joins = (W.wide_timing_query("wide_attn_decode_kvq" + x)[1]
+                                    for x in ("", "/runs", "/rows", "_merge"))
+    finally:
+        W.wide_timing_enable(False)
+    return every - runs - rows, runs, rows, joins
+
+
+@pytest.mark.parametrize("qg", [32, 64, 128])
+@pytest.mark.parametrize("B,L,n_q,n_kv,group,hm,cut", [
+    (3, 2200, 8, 2, 512, True, "runs"),        # 4 query heads per KV head
+    (2, 2081, 64, 8, 1024, True, "runs"),      # 8
+    (3, 2500, 10, 2, 640, True, "runs"),       # 5
+    (3, 2200, 16, 1, 1024, True, "runs"),      # 16
+    (3, 2081, 18, 2, 384, True, "runs"),       # 9
+    (2, 2300, 22, 2, 256, True, "runs"),       # 11
+    (2, 2081, 64, 8, 512, False, "runs"),
+    (3, 2200, 20, 4, 640, False, "runs"),
+    (3, 2081, 32, 2, 2048, False, "runs"),
+    (2, 2200, 39, 3, 384, False, "runs"),
+    (32, 2081, 64, 4, 2048, False, "rows"),
+    (32, 2081, 32, 4, 1024, False, "rows"),
+    (70, 2049, 6, 3, 384, False, "runs"),      # (one head group over two KV heads)
+    (180, 2049, 9, 3, 384, False, "pairs"),    # more than 512 pairs
+])
+def test_attention_long_by_heads(B, L, n_q, n_kv, group, hm, cut, qg):
+    """Contexts past 2048 keys for every number of query heads a KV head has columns for, ragged and
+    partly masked, with NaN behind the ends, and the kernel that is meant."""
+    say("long", B, L, n_q, n_kv, group, hm, cut, qg)
+    g = np.random.default_rng(B + n_q + qg)
+    q = rows_f64(n_q, (B, n_q * HD), torch.bfloat16, spread=0.3)
+    mask = (g.random((B, n_q * HD // group)) < 0.6).astype(np.uint8)
+    mask[0] = 1
+    kv_len = np.minimum(g.integers(0, L + 400, B) // (1 if B < 8 else 8), L)
+    kv_len[:2] = L, L - 35
+    few = min(B, 4)                                              # sequences with values of their own
+    kc, vc = (np.concatenate([c] * -(-B // few))[:B] for c in make_cache(n_q, few, L, n_kv, qg, hm))
+    kd, vd = (d(poison(c, kv_len, mask, n_q, n_kv, group, hm)) for c in (kc, vc))
+    args = (q.cuda(), kd, vd, d(mask), n_q, n_kv, group, qg, i32(kv_len), hm)
+    ws = torch.full((W.wide_attention_decode_kvq_workspace_size(B, L, n_q, n_kv, HD, group, qg),), 0xff,
+                    dtype=torch.uint8, device="cuda")
+    got = []
+    ran = kernels_of(lambda: got.append(run_attention(*args, ws=ws)))
+    assert ran == {"pairs": (1, 0, 0, 0), "runs": (0, 1, 0, 1), "rows": (0, 0, 1, 1)}[cut]
+    check_attention(got[0], q, kc, vc, mask, n_q, n_kv, group, qg, kv_len, hm, (B, L, n_q, n_kv, qg))
+    assert torch.equal(got[0].view(torch.int16), run_attention(*args).view(torch.int16))
+
+
 @pytest.mark.parametrize("n_kv,hm", [(8, True), (9, False)])
 def test_attention_more_pairs_than_a_launch_holds(n_kv, hm):
     """2^23 and more (sequence, KV head) pairs: more threads than one launch takes.  With one key the
@@ -582,6 +635,83 @@ def test_two_streams():
         for st, q, o in zip(streams, qs, out):
             with torch.cuda.stream(st):
                 run_attention(q, kc, vc, mask, n_q, n_kv, group, qg, None, hm, o=o)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("B,L,n_q,n_kv,group,qg,hm,cut", [
+    (4, 2300, 8, 2, 512, 32, True, (0, 1, 0, 1)),
+    (18, 4097, 16, 4, 512, 64, False, (0, 0, 1, 1)),
+])
+def test_graph_of_a_long_decode_step(B, L, n_q, n_kv, group, qg, hm, cut):
+    """The same over contexts whose work is cut and joined: two launches, and a workspace of NaN bytes
+    before each replay.  Sequences, KV heads and, once, the whole batch have nothing to attend to."""
+    say("graph", B, L, n_q, n_kv, group, qg, hm)
+    few = min(B, 4)
+    kc, vc = (d(np.concatenate([c] * -(-B // few))[:B]) for c in make_cache(4, few, L, n_kv, qg, hm))
+    k, v = (torch.zeros(B, n_kv * HD, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = torch.zeros(B, n_q * HD, dtype=torch.bfloat16, device="cuda")
+    pos, lens = (torch.zeros(B, dtype=torch.int32, device="cuda") for _ in range(2))
+    mask = torch.ones(B, n_q * HD // group, dtype=torch.uint8, device="cuda")
+    o = torch.empty_like(q)
+    ws = torch.empty(W.wide_attention_decode_kvq_workspace_size(B, L, n_q, n_kv, HD, group, qg), dtype=torch.uint8,
+                     device="cuda")
+
+    def step():
+        W.wide_kv_quantize(k, v, kc, vc, n_kv, HD, qg, pos=pos, kv_len=lens, head_major=hm)
+        run_attention(q, kc, vc, mask, n_q, n_kv, group, qg, lens, hm, o=o, ws=ws)
+
+    assert kernels_of(step) == cut
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    g = np.random.default_rng(B)
+    for n in range(5):
+        at = g.integers(0, L, B)
+        at[n % B], at[(n + 1) % B], at[(n + 2) % B] = L - 1, -1, 0       # the last place, nothing, one key
+        m = (g.random(mask.shape) < 0.6).astype(np.uint8)
+        m[(n + 3) % B] = 0
+        if n == 2:
+            at[:] = -1
+        if n == 3:
+            m[:] = 0
+        k.copy_(rows_f64(n, k.shape, torch.bfloat16, spread=0.2).cuda())
+        v.copy_(rows_f64(n + 50, k.shape, torch.bfloat16, spread=0.2).cuda())
+        qh = rows_f64(n + 90, q.shape, torch.bfloat16, spread=0.2)
+        q.copy_(qh.cuda())
+        pos.copy_(i32(at))
+        lens.copy_(i32(at + 1))
+        mask.copy_(d(m))
+        ws.fill_(0xff)
+        o.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = o.clone()
+        check_attention(got, qh, kc.cpu().numpy(), vc.cpu().numpy(), m, n_q, n_kv, group, qg, at + 1, hm, n)
+        ws.fill_(0xff)
+        step()                                                 # the same, eagerly
+        assert torch.equal(o.view(torch.int16), got.view(torch.int16))
+
+
+def test_two_streams_over_whole_rows():
+    """As test_two_streams, by the kernel that reads a position's rows whole."""
+    B, L, n_q, n_kv, group, qg = 18, 4097, 16, 4, 512, 32
+    kc, vc = (d(np.concatenate([c] * 9)) for c in make_cache(6, 2, L, n_kv, qg, False))
+    mask = torch.ones(B, n_q * HD // group, dtype=torch.uint8, device="cuda")
+    lens = [i32(np.random.default_rng(s).integers(0, L + 1, B)) for s in range(2)]
+    qs = [rows_f64(s, (B, n_q * HD), torch.bfloat16, spread=0.2).cuda() for s in range(2)]
+    args = [(q, kc, vc, mask, n_q, n_kv, group, qg, n, False) for q, n in zip(qs, lens)]
+    want = []
+    assert kernels_of(lambda: want.extend(run_attention(*a) for a in args)) == (0, 0, 2, 2)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    out = [torch.zeros_like(q) for q in qs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, a, o in zip(streams, args, out):
+            with torch.cuda.stream(st):
+                run_attention(*a, o=o)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(out, want))
 
