@@ -290,6 +290,21 @@ def test_attention_large_scores_and_not_finite_keys():
     assert torch.equal(o, o2)
 
 
+@pytest.mark.parametrize("qg", [32, 64, 128])
+@pytest.mark.parametrize("n_q", [8, 16, 32])
+@pytest.mark.parametrize("eq,ek,ev", [(0, 0, -110), (0, 0, -119), (110, -110, 0), (-110, 97, 0), (-125, -100, 97)])
+def test_attention_far_sizes(eq, ek, ev, n_q, qg):
+    """q, K and V of about 2^eq, 2^ek and 2^ev."""
+    B, L, n_kv, group, hm = 2, 130, 2, 512, True
+    say("sizes", eq, ek, ev, n_q, qg)
+    q = (rows_f64(1, (B, n_q * HD), torch.float32, spread=0.3) * 2.0 ** eq).bfloat16()
+    kc, vc = (_kvq.quantize(rows_f64(s, (B, n_kv, L, HD), torch.float32, spread=0.2).double().numpy() * 2.0 ** e, qg)
+              for s, e in ((2, ek), (3, ev)))
+    mask = np.ones((B, n_q * HD // group), np.uint8)
+    o = run_attention(q.cuda(), d(kc), d(vc), d(mask), n_q, n_kv, group, qg, None, hm)
+    check_attention(o, q, kc, vc, mask, n_q, n_kv, group, qg, None, hm, (eq, ek, ev))
+
+
 @pytest.mark.parametrize("B,L,n_q,n_kv,group,qg,hm,ragged", [
     (1, 9001, 8, 2, 512, 32, True, False),     # one long sequence: the keys are cut
     (2, 5000, 4, 4, 128, 128, False, True),
