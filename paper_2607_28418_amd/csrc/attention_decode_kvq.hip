@@ -39,10 +39,15 @@
 //
 // Bound by the cache's bytes (32 x 8192 keys, 8 KV heads, groups of 32, head-major:
 // 336 MB in 67 us with its join, 5.0 TB/s; 64 ragged ones of up to 32768, groups of
-// 64: 1.2 GB in 223, 5.4; a pure read of the same shape 6.1), short calls by latency
-// (500 keys: 6.3 us).  A tile is 175 vector instructions; two in flight a wave
+// 64: 1.2 GB in 227, 5.3; a pure read of the same shape 6.1), short calls by latency
+// (500 keys: 6.8 us).  A tile is 175 vector instructions; two in flight a wave
 // (three or four, or two computed together, cost 1-2 us a call in code and in loads
-// past the end).
+// past the end).  More query heads per KV head are bound by the sets: each multiplies
+// 128 deep with zeros outside its groups and keeps its own q (32 x 8192 keys, 32
+// query heads, groups of 32, 64, 128: 8 per KV head 44, 44 and 41 us for bytes that
+// a read takes 27, 24 and 23 for; 16 per KV head 48, 35, 34 for 14, 12, 12).  With 16
+// and groups of 32 the registers run out: 37 of a lane are spilled (23 in the kernel
+// of a workgroup per pair), accesses inside the loop over tiles among them.
 #include <algorithm>
 
 #include "common.h"
@@ -548,7 +553,7 @@ __global__ __launch_bounds__(kSplitThreads, 2) void wide_attn_decode_kvq_runs(At
 // a line each, so heads read one by one, 1.6 lines for 80 bytes, get little more
 // than half of the rate (32 x 8192 keys, 8 KV heads: 98 us; 122 with the heads of a
 // position on different XCDs, too, so that each fetches the line).  Here a
-// workgroup of eight waves reads whole runs of rows for eight heads into LDS (75 us),
+// workgroup of eight waves reads whole runs of rows for eight heads into LDS (71 us),
 // or for four or two, the largest number that divides the heads.
 //
 // A unit of work is (sequence, eight KV heads, run of stages); a stage is 256 rows:
@@ -556,8 +561,9 @@ __global__ __launch_bounds__(kSplitThreads, 2) void wide_attn_decode_kvq_runs(At
 // four positions) are a super-row, 8 R bytes; wave w of the first four loads super-rows 8 w .. 8 w + 7 of
 // K, the others of V, in 16-byte chunks, direct to LDS, two stages ahead, leaving
 // out chunks of inactive heads; then wave w attends for head w mod heads over the
-// 32 positions of part w / heads.  The units of a sequence take q stages each, the
-// least q for which all of them fit the workgroups.
+// 32 positions of part w / heads.  The units of a sequence take q stages each, q the
+// least of 64 candidates, from the mean to where the units are sure to fit, for
+// which all of them fit the workgroups.
 template <int NG>
 struct RowStage {
   static constexpr int R = 64 + 4 * NG, SUPER = 8 * R;
@@ -948,8 +954,15 @@ constexpr int kMany = 512;   // pairs
 //    138.  With more than 512 groups each workgroup spends too long on the list: 900
 //    sequences of 2100 682, a workgroup per pair 616; 600 of them 393 and 411;
 //  - other token-major caches of more than 512 pairs: a workgroup per pair, whose
-//    neighbours read the same lines at about the same time (200 sequences of 4096,
-//    3 KV heads: 108, as runs 146);
+//    neighbours read the same lines at about the same time.  Which is better depends
+//    on the lengths and the mask, not known here; the border is where what one side
+//    gains with full sequences the other gains with ragged, half-masked ones.  3 KV
+//    heads, a workgroup per pair and runs, full; ragged; ragged and half masked:
+//      255 pairs, 16384 keys: 148 and 223; 126 and 121; 135 and 65
+//      510 pairs, 4096 keys: 84 and 117; 63 and 68; 54 and 40
+//      510 pairs, 16384 keys: 309 and 430; 227 and 236; 191 and 123
+//      639 pairs, 16384 keys: 422 and 646; 272 and 293; 235 and 154
+//      999 pairs, 16384 keys: 589 and 859; 378 and 464; 280 and 243;
 //  - else runs.
 KvqPlan attn_decode_kvq_plan(int64_t B, int n_kv, int L, int qpk, bool head_major, bool whole) {
   KvqPlan p{};
